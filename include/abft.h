@@ -5,7 +5,8 @@
  * (fully-connected layers and convolutions lowered to a matrix product) and checks
  * the result with algorithm-based fault tolerance, following Kosaian & Rashmi,
  * "Arithmetic-Intensity-Guided Fault Tolerance for Neural Network Inference on
- * GPUs" (SC '21).  Notation is the paper's (Sec. 2.1): A is M x K (activations),
+ * GPUs" (SC '21).  For language models it also holds what stands between such products when their
+ * weights are int8: quantised linear layers and a paged cache of keys and values.  Notation is the paper's (Sec. 2.1): A is M x K (activations),
  * B is K x N (weights, known before inference), C is M x N.
  *
  * General conventions
@@ -46,6 +47,7 @@ extern "C" {
 #define ABFT_E_HIP (-7)        /* a HIP runtime call failed (launch, allocation) */
 #define ABFT_E_PLAN (-8)       /* bad plan handle or layer index */
 #define ABFT_E_UNSUPPORTED (-9) /* the scheme is not available for this product (see ABFT_GLOBAL_WEIGHTED) */
+#define ABFT_E_VALUE (-10)     /* a scale, window or page size is out of its range */
 
 /* ---- enums --------------------------------------------------------------- */
 /* Protection scheme.  GLOBAL: kernel-level ABFT (Sec. 2.4-2.5): the weight checksums are
@@ -433,6 +435,71 @@ int abft_plan_mode(const abft_plan_t *plan, int layer);
  * THREAD (zeros when profile = 0). */
 int abft_plan_times(const abft_plan_t *plan, int layer, double *out3 /* host */);
 void abft_plan_destroy(abft_plan_t *plan);
+
+/* ---- int8 linear layers of 16-bit activations ------------------------------- */
+/* Quantise the rows of X (M x K, row-major, ldx >= K, F16 or BF16, any alignment), one token's activations each, to
+ * int8: with a = max over the row of |x|,
+ *     scale[m] = a / 127 (float),   Q[m][k] = 127 x / a rounded to nearest, halves away from zero
+ * exactly (|Q| <= 127).  A row of zeros has the scale 0; a row that holds an infinity or a NaN has the scale NaN and Q = 0, so
+ * that what is computed from it is NaN.  Q: M x K int8, ldq >= K.  One launch, no workspace. */
+int abft_quantize_rows(int M, int K, const void *X, int64_t ldx, int dtype, void *Q, int64_t ldq, float *scale,
+                       void *stream);
+
+/* C = act((A.B) * row_scale * col_scale + bias): an int8 product whose int32 sums leave as 16-bit values.
+ *   A, B, ldb, b_layout, beta, workspace, fault_flag, report, inject: as for abft_gemm with ABFT_I8 (regions, tiles and workspace
+ *       of that product: abft_region_shape, abft_workspace_bytes).  A: M x K int8.  The checks see the int32 sums and compare
+ *       exactly, as they do there.
+ *   row_scale: M floats (abft_quantize_rows); col_scale: N floats; bias: N floats or NULL.
+ *   act: abft_act_t.  C: M x N, ldc >= N, of type out_dtype (F16 / BF16).  C[m][n] is the sum as a float, times row_scale[m], times
+ *       col_scale[n] plus bias[n] in one fused step, after the activation function, rounded once to nearest even.
+ *   mode: ABFT_NONE, ABFT_GLOBAL, ABFT_THREAD, or ABFT_AUTO (abft_select for ABFT_I8); the others: ABFT_E_UNSUPPORTED.
+ *   K: at most 131071 (the sums stay within int32), else ABFT_E_SHAPE. */
+int abft_gemm_scaled(int M, int N, int K, const void *A, int64_t lda, const float *row_scale, const void *B, int64_t ldb,
+                     int b_layout, const float *col_scale, const float *bias, int act, void *C, int64_t ldc, int out_dtype,
+                     int mode, const void *beta, void *workspace, size_t workspace_bytes, uint32_t *fault_flag,
+                     abft_report_t *report, const abft_fault_t *inject, void *stream);
+
+/* The two in one call: a linear layer of 16-bit activations X (M x K, ldx >= K, F16 / BF16) and int8 weights B with a
+ * scale per output channel; C has the type of X.  The quantised activations and their scales live in the workspace (256-byte
+ * aligned, abft_linear_scaled_workspace_bytes bytes, whatever the mode; no initialisation), in rows padded to whole
+ * chunks: `aligned` of abft_region_shape is K % 16 == 0 and an aligned B in ABFT_B_NK order.  Results are those of
+ * abft_quantize_rows and abft_gemm_scaled.  What is refused is refused before anything is launched. */
+int abft_linear_scaled(int M, int N, int K, const void *X, int64_t ldx, int dtype, const void *B, int64_t ldb, int b_layout,
+                       const float *col_scale, const float *bias, int act, void *C, int64_t ldc, int mode, const void *beta,
+                       void *workspace, size_t workspace_bytes, uint32_t *fault_flag, abft_report_t *report,
+                       const abft_fault_t *inject, void *stream);
+/* Bytes of workspace abft_linear_scaled wants (0 for invalid arguments). */
+size_t abft_linear_scaled_workspace_bytes(int M, int N, int K, int mode);
+
+/* ---- a paged cache of keys and values ----------------------------------------- */
+/* The cache of one attention layer: `pages` pages of `page_size` tokens.  A token's place is a slot,
+ * page * page_size + its offset in the page; which pages a sequence has, in order, is the caller's block table.
+ *   k, v            : pages x heads x page_size x head_dim, 16-byte aligned
+ *   k_scale, v_scale: pages x heads x page_size floats; ABFT_I8 only, else NULL
+ *   dtype           : ABFT_I8 (integers with a scale for each token and head, the rule of abft_quantize_rows over
+ *                     head_dim values), or ABFT_F16 / ABFT_BF16 (the values as they are)
+ *   page_size       : a multiple of 16 up to 4096 (ABFT_E_VALUE); pages * page_size below 2^31
+ *   head_dim        : a multiple of 16 up to 128 (ABFT_E_SHAPE)
+ * The struct is read during a call only; the buffers are the caller's. */
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int32_t dtype;
+    int32_t pages, page_size, heads, head_dim;
+} abft_kv_cache_t;
+
+/* Write keys and values of new tokens into their slots, quantised on the way if the cache is int8.
+ *   slots: `tokens` int64 (device).  A negative slot, or one beyond the cache, is passed over.  No slot may be given twice
+ *          in a call.
+ *   K, V : token t's heads * head_dim values at K + t * ldk (elements, ldk >= heads * head_dim; any alignment: columns
+ *          of a larger product as they are), F16 / BF16; a 16-bit cache takes its own type only (ABFT_E_ENUM).
+ * tokens = 0 is a call that does nothing. */
+int abft_kv_write(const abft_kv_cache_t *cache /* host */, int tokens, const int64_t *slots, const void *K, int64_t ldk,
+                  const void *V, int64_t ldv, int dtype, void *stream);
+/* The way back: K and V receive the slots' values (integer times scale, rounded to dtype); a slot outside the cache reads
+ * zeros.  Layout, types and checks as for abft_kv_write. */
+int abft_kv_read(const abft_kv_cache_t *cache /* host */, int tokens, const int64_t *slots, void *K, int64_t ldk, void *V,
+                 int64_t ldv, int dtype, void *stream);
 
 /* ---- misc ------------------------------------------------------------------ */
 const char *abft_strerror(int code);

@@ -51,6 +51,12 @@ class Layer(ctypes.Structure):
                 ("conv", Conv), ("B", ctypes.c_void_p), ("ldb", ctypes.c_int64)]
 
 
+class KVCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("dtype", ctypes.c_int32), ("pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32)]
+
+
 EXPORTS = [
     "abft_gemm", "abft_conv", "abft_workspace_bytes", "abft_weight_checksum",
     "abft_activation_checksum", "abft_arithmetic_intensity", "abft_cmr", "abft_set_cmr",
@@ -61,6 +67,8 @@ EXPORTS = [
     "abft_plan_set_activation", "abft_plan_activation", "abft_gemm_static", "abft_static_scratch_bytes",
     "abft_tolerance_half_coeff", "abft_plan_run_chain", "abft_plan_chain_status", "abft_plan_chain_reset",
     "abft_plan_set_diagnostics", "abft_kernel_name", "abft_handover_launches", "abft_chain_launches", "abft_shared_launches", "abft_mfma_probe", "abft_mfma_probe_bytes",
+    "abft_quantize_rows", "abft_gemm_scaled", "abft_linear_scaled", "abft_linear_scaled_workspace_bytes",
+    "abft_kv_write", "abft_kv_read",
 ]
 
 _lib = None
@@ -163,6 +171,20 @@ def lib() -> ctypes.CDLL:
     L.abft_version.argtypes = []
     L.abft_set_kernel_events.restype = None
     L.abft_set_kernel_events.argtypes = [vp, vp]
+    L.abft_quantize_rows.restype = ci
+    L.abft_quantize_rows.argtypes = [ci, ci, vp, i64, ci, vp, i64, vp, vp]
+    L.abft_gemm_scaled.restype = ci
+    L.abft_gemm_scaled.argtypes = [ci, ci, ci, vp, i64, vp, vp, i64, ci, vp, vp, ci, vp, i64, ci, ci, vp, vp, sz, vp, vp,
+                                   ctypes.POINTER(Fault), vp]
+    L.abft_linear_scaled.restype = ci
+    L.abft_linear_scaled.argtypes = [ci, ci, ci, vp, i64, ci, vp, i64, ci, vp, vp, ci, vp, i64, ci, vp, vp, sz, vp, vp,
+                                     ctypes.POINTER(Fault), vp]
+    L.abft_linear_scaled_workspace_bytes.restype = sz
+    L.abft_linear_scaled_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    cp = ctypes.POINTER(KVCache)
+    for f in (L.abft_kv_write, L.abft_kv_read):
+        f.restype = ci
+        f.argtypes = [cp, ci, vp, vp, i64, vp, i64, ci, vp]
     _lib = L
     return L
 
@@ -427,3 +449,41 @@ def abft_plan_destroy(plan) -> None:
 def abft_set_kernel_events(start_event, stop_event) -> None:
     """hipEvent_t handles (ints) recorded around the matrix-product kernel; None, None = off."""
     lib().abft_set_kernel_events(start_event, stop_event)
+
+
+def abft_quantize_rows(M, K, X, ldx, dtype, Q, ldq, scale, stream=None) -> None:
+    _check(lib().abft_quantize_rows(M, K, _ptr(X), ldx, dtype, _ptr(Q), ldq, _ptr(scale), _stream(stream)))
+
+
+def abft_gemm_scaled(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, beta=None,
+                     workspace=None, workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None,
+                     stream=None) -> None:
+    ip = ctypes.byref(inject) if inject is not None else None
+    _check(lib().abft_gemm_scaled(M, N, K, _ptr(A), lda, _ptr(row_scale), _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act,
+                                  _ptr(C), ldc, out_dtype, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag),
+                                  _ptr(report), ip, _stream(stream)))
+
+
+def abft_linear_scaled(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, C, ldc, mode, beta=None, workspace=None,
+                       workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None, stream=None) -> None:
+    ip = ctypes.byref(inject) if inject is not None else None
+    _check(lib().abft_linear_scaled(M, N, K, _ptr(X), ldx, dtype, _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act, _ptr(C),
+                                    ldc, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag), _ptr(report), ip,
+                                    _stream(stream)))
+
+
+def abft_linear_scaled_workspace_bytes(M, N, K, mode) -> int:
+    return lib().abft_linear_scaled_workspace_bytes(M, N, K, mode)
+
+
+def kv_cache(k, v, k_scale, v_scale, dtype, pages, page_size, heads, head_dim) -> KVCache:
+    """The descriptor of a cache (tensors or pointers; they must outlive it)."""
+    return KVCache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), dtype, pages, page_size, heads, head_dim)
+
+
+def abft_kv_write(cache: KVCache, tokens, slots, K, ldk, V, ldv, dtype, stream=None) -> None:
+    _check(lib().abft_kv_write(ctypes.byref(cache), tokens, _ptr(slots), _ptr(K), ldk, _ptr(V), ldv, dtype, _stream(stream)))
+
+
+def abft_kv_read(cache: KVCache, tokens, slots, K, ldk, V, ldv, dtype, stream=None) -> None:
+    _check(lib().abft_kv_read(ctypes.byref(cache), tokens, _ptr(slots), _ptr(K), ldk, _ptr(V), ldv, dtype, _stream(stream)))

@@ -19,6 +19,7 @@
 #include "gemm_configs.h"
 #include "mlp_chain.h"
 #include "gemm_group.h"
+#include "quantize.h"
 
 using namespace abft;
 
@@ -720,6 +721,9 @@ struct Problem {
     long long ld_alpha_out;
     bool* alpha_emitted;
     const float* alpha_in;
+    // scaled int8 product (row_scale not null): the type C is stored in, its scales, a bias or null
+    int out_dtype;
+    const float *row_scale, *col_scale, *bias;
 };
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -990,6 +994,57 @@ bool shallow_takes(const Problem& pr, int cfg, int mode) {
     return cfg == CFG_G64 && (mode == ABFT_NONE || mode == ABFT_THREAD) && !pr.conv && pr.b_layout == ABFT_B_NK && kb >= 16 && kb <= 128;
 }
 
+size_t plain_workspace_bytes(int M, int N, int K, int dtype, int mode);
+
+// ---- int8 products of 16-bit activations ----
+constexpr int SCALED_MAX_K = (1 << 17) - 1;
+int validate_quantize(int M, int K, const void* X, long long ldx, int dtype) {
+    if (dtype != ABFT_F16 && dtype != ABFT_BF16) return ABFT_E_ENUM;
+    if (M <= 0 || K <= 0) return ABFT_E_SHAPE;
+    if (!X) return ABFT_E_NULL;
+    if (ldx < K) return ABFT_E_LD;
+    return ABFT_OK;
+}
+hipError_t quantize_rows(int M, int K, const void* X, long long ldx, int dtype, void* Q, long long ldq, float* scale, hipStream_t st) {
+    QuantizeArgs a;
+    a.X = reinterpret_cast<const char*>(X);
+    a.Q = reinterpret_cast<signed char*>(Q);
+    a.scale = scale;
+    a.M = M; a.K = K; a.ldx = ldx; a.ldq = ldq;
+    return dtype == ABFT_F16 ? launch_quantize_rows<DT_F16>(a, st) : launch_quantize_rows<DT_BF16>(a, st);
+}
+// A scaled product as a problem, checked as far as it is more than one in int8.  K: beyond it 128 * 128 * K passes an int32.
+int scaled_problem(int M, int N, int K, const void* A, long long lda, const float* row_scale, const void* B, long long ldb, int b_layout,
+                   const float* col_scale, const float* bias, int act, void* C, long long ldc, int out_dtype, int mode, const uint32_t* flag,
+                   Problem& pr) {
+    std::memset(&pr, 0, sizeof pr);
+    pr.M = M; pr.N = N; pr.K = K; pr.dtype = ABFT_I8; pr.b_layout = b_layout;
+    pr.A = A; pr.lda = lda; pr.B = B; pr.ldb = ldb; pr.C = C; pr.ldc = ldc;
+    pr.act = act; pr.out_dtype = out_dtype;
+    pr.row_scale = row_scale; pr.col_scale = col_scale; pr.bias = bias;
+    if (out_dtype != ABFT_F16 && out_dtype != ABFT_BF16) return ABFT_E_ENUM;
+    if (act != ABFT_ACT_NONE && act != ABFT_ACT_RELU) return ABFT_E_ENUM;
+    if (!row_scale || !col_scale) return ABFT_E_NULL;
+    if (K > SCALED_MAX_K) return ABFT_E_SHAPE;
+    const int rc = validate_common(pr, mode, flag);
+    if (rc != ABFT_OK) return rc;
+    return mode == ABFT_NONE || mode == ABFT_GLOBAL || mode == ABFT_THREAD || mode == ABFT_AUTO ? ABFT_OK : ABFT_E_UNSUPPORTED;
+}
+// where a linear layer's workspace holds the quantised activations (rows of whole 16-byte chunks, at its start), their scales, and
+// what the product wants
+long long linear_ld(int K) { return (long long)align_up((size_t)K, 16); }
+size_t linear_scale_offset(int M, int K) { return align_up((size_t)M * linear_ld(K), 256); }
+size_t linear_product_offset(int M, int K) { return linear_scale_offset(M, K) + align_up((size_t)M * 4, 256); }
+
+// the k granularity of a fault that is planted in the loop, and whether a fault lies inside the product
+bool inject_in_range(const Problem& pr, int mode, const abft_fault_t& f) {
+    if (mode == ABFT_AUTO) mode = select_mode(pr.M, pr.N, pr.K, pr.dtype);
+    const int cfg = pick_cfg(pr.M, pr.N, pr.K, pr.dtype, a_vectorisable(pr) && b_vectorisable(pr), mode, pr.conv);
+    const int bk = cfg_info_host(cfg).bk_bytes / esize(pr.dtype);
+    if (f.row < 0 || f.row >= pr.M || f.col < 0 || f.col >= pr.N || f.bit < 0 || f.bit > 31 || f.k_after < -2) return false;
+    return f.k_after < 0 || (f.k_after != 0 && f.k_after % bk == 0 && f.k_after < pr.K);
+}
+
 // A product ready to be launched
 struct Prepared {
     GemmArgs g;
@@ -1038,6 +1093,7 @@ int prepare_problem(const Problem& pr, int mode, const void* beta, void* workspa
     g.tiles_n = (int)cdiv(pr.N, ci.bn);
     g.flag = flag;
     g.act = pr.act;
+    g.row_scale = pr.row_scale; g.col_scale = pr.col_scale; g.bias = pr.bias;
     g.report = reinterpret_cast<Report*>(report);
     const int tol_K = pr.tol_K > 0 ? pr.tol_K : pr.K;
     g.tol_coeff = tol_coeff(tol_K, pr.dtype, mode) + tol_half_coeff(pr.dtype, mode, ci.wm, ci.wn, cfg == CFG_G16 ? 16 : 32);
@@ -1112,7 +1168,7 @@ int prepare_problem(const Problem& pr, int mode, const void* beta, void* workspa
     out.dtype = pr.dtype;
     out.inj = inj;
     const long long blocks = (long long)g.tiles_m * g.tiles_n;
-    out.shallow = !inj && !g.alpha_out && shallow_takes(pr, cfg, mode) && blocks <= 512 &&
+    out.shallow = !inj && !g.alpha_out && !pr.row_scale && shallow_takes(pr, cfg, mode) && blocks <= 512 &&
                   (long long)pr.K * esize(pr.dtype) <= (blocks > 256 && rows_off_dwords(g, pr.dtype) ? 64 : 96);
     out.skinny = !g.alpha_out && skinny_takes(pr, cfg, mode);
     if (out.skinny) {
@@ -1131,7 +1187,11 @@ int run_problem(const Problem& pr, int mode, const void* beta, void* workspace, 
     if (rc != ABFT_OK) return rc;
     hipError_t e;
     if (g_ev_start && hipEventRecord(g_ev_start, st) != hipSuccess) return ABFT_E_HIP;
-    if (w.skinny) {
+    if (pr.row_scale) {
+        const bool f16 = pr.out_dtype == ABFT_F16;
+        if (w.skinny) e = (f16 ? launch_scaled_skinny_f16 : launch_scaled_skinny_bf16)(w.kmode, rows_off_dwords(w.g, w.dtype), cfg_info_host(w.cfg).wn, w.g, st);
+        else e = f16 ? launch_scaled_f16(w.cfg, w.kmode, w.inj, w.g, st) : launch_scaled_bf16(w.cfg, w.kmode, w.inj, w.g, st);
+    } else if (w.skinny) {
         const int columns = cfg_info_host(w.cfg).wn;
         e = w.dtype == ABFT_F16    ? launch_skinny_f16(w.kmode, rows_off_dwords(w.g, w.dtype), columns, w.g, st)
             : w.dtype == ABFT_BF16 ? launch_skinny_bf16(w.kmode, rows_off_dwords(w.g, w.dtype), columns, w.g, st)
@@ -1209,7 +1269,6 @@ ConvLowering conv_lowering(const Problem& pr) {
     return lw;
 }
 
-size_t plain_workspace_bytes(int M, int N, int K, int dtype, int mode);
 
 // bytes of workspace that let a convolution run lowered: the lowered product's own scratch, the
 // padded input, the re-ordered weights
@@ -1410,6 +1469,51 @@ int abft_gemm_static(int M, int N, int K, const void* A, int64_t lda, const void
     // (a product whose scratch does not fit comes back as ABFT_E_WORKSPACE before anything is launched)
     return run_problem(pr, mode, beta, scratch, STATIC_SCRATCH_BYTES, fault_flag, report, inject,
                        reinterpret_cast<hipStream_t>(stream));
+}
+
+int abft_quantize_rows(int M, int K, const void* X, int64_t ldx, int dtype, void* Q, int64_t ldq, float* scale, void* stream) {
+    const int rc = validate_quantize(M, K, X, ldx, dtype);
+    if (rc != ABFT_OK) return rc;
+    if (!Q || !scale) return ABFT_E_NULL;
+    if (ldq < K) return ABFT_E_LD;
+    return quantize_rows(M, K, X, ldx, dtype, Q, ldq, scale, reinterpret_cast<hipStream_t>(stream)) == hipSuccess ? ABFT_OK : ABFT_E_HIP;
+}
+
+int abft_gemm_scaled(int M, int N, int K, const void* A, int64_t lda, const float* row_scale, const void* B, int64_t ldb, int b_layout,
+                     const float* col_scale, const float* bias, int act, void* C, int64_t ldc, int out_dtype, int mode, const void* beta,
+                     void* workspace, size_t workspace_bytes, uint32_t* fault_flag, abft_report_t* report, const abft_fault_t* inject,
+                     void* stream) {
+    Problem pr;
+    const int rc = scaled_problem(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, fault_flag, pr);
+    if (rc != ABFT_OK) return rc;
+    return run_problem(pr, mode, beta, workspace, workspace_bytes, fault_flag, report, inject, reinterpret_cast<hipStream_t>(stream));
+}
+
+size_t abft_linear_scaled_workspace_bytes(int M, int N, int K, int mode) {
+    if (M <= 0 || N <= 0 || K <= 0) return 0;
+    return linear_product_offset(M, K) + plain_workspace_bytes(M, N, K, ABFT_I8, mode);
+}
+
+int abft_linear_scaled(int M, int N, int K, const void* X, int64_t ldx, int dtype, const void* B, int64_t ldb, int b_layout,
+                       const float* col_scale, const float* bias, int act, void* C, int64_t ldc, int mode, const void* beta,
+                       void* workspace, size_t workspace_bytes, uint32_t* fault_flag, abft_report_t* report, const abft_fault_t* inject,
+                       void* stream) {
+    int rc = validate_quantize(M, K, X, ldx, dtype);
+    if (rc != ABFT_OK) return rc;
+    const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    char* const ws = reinterpret_cast<char*>(workspace);
+    const size_t product = linear_product_offset(M, K);
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || workspace_bytes < product) return ABFT_E_WORKSPACE;
+    float* const row_scale = reinterpret_cast<float*>(ws + linear_scale_offset(M, K));
+    Problem pr;
+    rc = scaled_problem(M, N, K, ws, linear_ld(K), row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, dtype, mode, fault_flag, pr);
+    if (rc != ABFT_OK) return rc;
+    // (everything that can be refused is, before the first launch)
+    const size_t left = workspace_bytes - product;
+    if (left < plain_workspace_bytes(M, N, K, ABFT_I8, mode)) return ABFT_E_WORKSPACE;
+    if (inject && !inject_in_range(pr, mode, *inject)) return ABFT_E_INJECT;
+    if (quantize_rows(M, K, X, ldx, dtype, ws, linear_ld(K), row_scale, st) != hipSuccess) return ABFT_E_HIP;
+    return run_problem(pr, mode, beta, left ? ws + product : nullptr, left, fault_flag, report, inject, st);
 }
 
 size_t abft_static_scratch_bytes(void) { return STATIC_SCRATCH_BYTES; }
@@ -2214,6 +2318,7 @@ const char* abft_strerror(int code) {
         case ABFT_E_HIP: return "HIP runtime call failed";
         case ABFT_E_PLAN: return "bad plan handle or layer index";
         case ABFT_E_UNSUPPORTED: return "scheme not available for this product";
+        case ABFT_E_VALUE: return "a scale, window or page size is out of its range";
     }
     return "unknown error code";
 }

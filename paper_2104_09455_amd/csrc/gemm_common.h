@@ -151,6 +151,8 @@ struct GemmArgs {
     // strip kernel (strip_pitch != 0): bytes of an input row and rows it keeps in LDS; elements of a filter
     // row's run in B where the channels fill no k tile (A is the input as it is, B and K are in that order)
     int strip_pitch, strip_rows, strip_seg;
+    // scaled int8 products (Cfg::SCALED): one scale per row and per column, and a bias per column or null
+    const float *row_scale, *col_scale, *bias;
 };
 
 template <typename To, typename Ti>
@@ -284,6 +286,8 @@ struct Cfg {
     static constexpr int WAVES_M = WAVES_M_, WAVES_N = WAVES_N_, BKB = BKB_;
     static constexpr int ESIZE = (DT_ == DT_I8) ? 1 : 2;  // bytes per input element
     static constexpr int CSIZE = (DT_ == DT_I8) ? 4 : 2;  // bytes per output element
+    static constexpr bool SCALED = false;                 // (ScaledCfg)
+    static constexpr int OUT = DT_;                       // the type that 16-bit outputs are stored in
     static constexpr int EPC = 16 / ESIZE;                // elements per 16-byte chunk
     static constexpr int WM = MI_ * TM_, WN = MI_ * TN_;  // wavefront register tile
     static constexpr int BM = WM * WAVES_M_, BN = WN * WAVES_N_;
@@ -303,6 +307,17 @@ struct Cfg {
     static_assert(THREADS % CPR == 0, "threads must cover whole tile rows");
     static_assert(BM % ROWS_PER_PASS == 0 && BN % ROWS_PER_PASS == 0, "tile rows vs threads");
     static_assert(BKB_ % Mma<DT_, MI_>::KBYTES == 0, "k tile vs MFMA depth");
+};
+
+// The same tiles for int8 operands whose results leave as 16-bit values: element (m, n) is its int32 sum (which the checks
+// see, exactly) times row_scale[m] times col_scale[n], plus bias[n], after the activation function, rounded once.
+// The sum becomes a float (one rounding beyond 2^24), and takes one scale after the other: their product alone could
+// underflow where the result does not.
+template <class BASE, int OUT_>
+struct ScaledCfg : BASE {
+    static_assert(BASE::DT == DT_I8 && OUT_ != DT_I8, "int8 in, 16 bits out");
+    static constexpr bool SCALED = true;
+    static constexpr int OUT = OUT_, CSIZE = 2;
 };
 
 __device__ __forceinline__ i32x4 ld16(const char* p) { return *reinterpret_cast<const i32x4*>(p); }
@@ -800,6 +815,44 @@ __device__ __forceinline__ bool cross_wave_last(char* epi, int lane, int wave) {
 __device__ __forceinline__ int relu(int x) { return x > 0 ? x : 0; }
 __device__ __forceinline__ float relu(float x) { return __builtin_amdgcn_fmed3f(x, 3.402823466e+38f, 0.f); }
 
+// One element of a scaled product, ready to be rounded
+__device__ __forceinline__ float scaled_value(int sum, float row, float col, float bias, int act) {
+    const float v = __builtin_fmaf((float)sum * row, col, bias);
+    return act ? relu(v) : v;
+}
+// The scales of up to four consecutive rows; rows outside C take the last one's
+__device__ __forceinline__ f32x4 row_scales(const GemmArgs& p, int row) {
+    if (row + 4 <= p.M) return load_global_unaligned<f32x4>(reinterpret_cast<const char*>(p.row_scale + row));
+    f32x4 s;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) s[r] = p.row_scale[min(row + r, p.M - 1)];
+    return s;
+}
+// The accumulators of a wavefront tile scaled in place: floats from here on
+template <class CFG>
+__device__ __forceinline__ void scale_tile(typename Mma<CFG::DT, CFG::MI>::Acc (&acc)[CFG::TM][CFG::TN], const GemmArgs& p,
+                                           const TileCoords<CFG>& tc) {
+    typedef Mma<CFG::DT, CFG::MI> MMA;
+    float col[CFG::TN], bias[CFG::TN];
+#pragma unroll
+    for (int j = 0; j < CFG::TN; ++j) {
+        const int n = min(tc.col(j), p.N - 1);
+        col[j] = p.col_scale[n];
+        bias[j] = p.bias ? p.bias[n] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < CFG::TM; ++i)
+#pragma unroll
+        for (int r = 0; r < MMA::NACC; r += 4) {
+            const f32x4 row = row_scales(p, tc.row(i, r));
+#pragma unroll
+            for (int j = 0; j < CFG::TN; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    acc[i][j][r + q] = bitcast<int>(scaled_value(acc[i][j][r + q], row[q], col[j], bias[j], p.act));
+        }
+}
+
 // Checksum epilogue (taken from the accumulators, before down-conversion) and store of C.
 //  GLOBAL: fused output summation (Sec. 2.5) of the workgroup tile, compared right here with
 //          the tile's checksum dot product (Sec. 2.4 steps 3-4).  lane_dot (a double, or a
@@ -1017,7 +1070,9 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
     }
 
     if (!store) return;
-    if (p.act) {
+    if constexpr (CFG::SCALED) {
+        scale_tile<CFG>(acc, p, tc);
+    } else if (p.act) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -1028,7 +1083,7 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
     // ---- activation checksums for the next layer: per 32-row block and column, the sum of the
     // values as they are stored (a lane holds 16 rows of one column of each MFMA block, the
     // lane 32 further on the other 16); rows past M hold zeros
-    if constexpr (CFG::CSIZE == 2 && MI == 32) {
+    if constexpr (!IS_INT && MI == 32) {
         if (p.alpha_out) {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
@@ -1049,7 +1104,7 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
                 }
         }
     }
-    if constexpr (CFG::CSIZE == 2 && MI == 16 && TM % 2 == 0) {
+    if constexpr (!IS_INT && MI == 16 && TM % 2 == 0) {
         // (16x16 shapes, direct-to-LDS kernel: a lane holds 4 rows of one column of each block; two
         // block rows make a 32-row block, the lanes 16, 32 and 48 further on hold its other rows)
         if (p.alpha_out) {
@@ -1074,7 +1129,9 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
                 }
         }
     }
-    // ---- store C (rounded to the output type)
+    // ---- store C (rounded to the output type; the accumulators of a scaled product hold floats by now)
+    auto value = [](auto v) { return bitcast<float>((typename MMA::AccT)v); };
+    (void)value;
     if constexpr (CFG::INTERLEAVED) {
         // A lane's TN adjacent columns at once, at whatever address its run of them starts, fewer where N cuts them.  By the
         // element, TN columns apart from lane to lane, tiles that C cuts and rows at odd addresses wrote a line in pieces (by the
@@ -1091,7 +1148,7 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
         struct __attribute__((packed, aligned(CFG::CSIZE))) AnyRun { Run v; };
         struct __attribute__((packed, aligned(CFG::CSIZE))) AnyPair { Pair v; };
         auto pair = [&](int i, int j, int r) -> Pair {
-            if constexpr (CFG::CSIZE == 2) return pack_out16<CFG::DT>(acc[i][j][r], acc[i][j + 1][r]);
+            if constexpr (CFG::CSIZE == 2) return pack_out16<CFG::OUT>(value(acc[i][j][r]), value(acc[i][j + 1][r]));
             else return Int2{acc[i][j][r], acc[i][j + 1][r]};
         };
         auto store_run = [&](char* dst, int i, int r) {
@@ -1179,8 +1236,8 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
                     for (int j = 0; j < TN; ++j)
-                        store_quad_rows<CFG::DT>(acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2],
-                                                 acc[i][j][4 * g + 3], base + (i * 32 + 8 * g) * ldcb + j * 64, lane);
+                        store_quad_rows<CFG::OUT>(value(acc[i][j][4 * g]), value(acc[i][j][4 * g + 1]), value(acc[i][j][4 * g + 2]),
+                                                  value(acc[i][j][4 * g + 3]), base + (i * 32 + 8 * g) * ldcb + j * 64, lane);
             return;
         }
     }
@@ -1194,8 +1251,8 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
                 const int row = acc_row(i, r);
                 if (row < M && col < N) {
                     char* dst = p.C + ((long long)row * p.ldc + col) * CFG::CSIZE;
-                    if constexpr (CFG::DT == DT_F16) *reinterpret_cast<_Float16*>(dst) = (_Float16)acc[i][j][r];
-                    else if constexpr (CFG::DT == DT_BF16) *reinterpret_cast<__bf16*>(dst) = (__bf16)acc[i][j][r];
+                    if constexpr (CFG::OUT == DT_F16) *reinterpret_cast<_Float16*>(dst) = (_Float16)value(acc[i][j][r]);
+                    else if constexpr (CFG::OUT == DT_BF16) *reinterpret_cast<__bf16*>(dst) = (__bf16)value(acc[i][j][r]);
                     else *reinterpret_cast<int*>(dst) = acc[i][j][r];
                 }
             }

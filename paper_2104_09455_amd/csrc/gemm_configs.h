@@ -136,4 +136,19 @@ ABFT_DECLARE_LAUNCHES(bf16)
 ABFT_DECLARE_LAUNCHES(i8)
 #undef ABFT_DECLARE_LAUNCHES
 
+// scaled int8 products: the same per output type, in gemm_scaled_<family>_<type>.hip
+#define ABFT_DECLARE_SCALED(out)                                                                                          \
+    hipError_t launch_scaled_fast_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);    \
+    hipError_t launch_scaled_stream_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);  \
+    hipError_t launch_scaled_generic_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream); \
+    hipError_t launch_scaled_skinny_##out(int mode, bool bytes, int columns, const GemmArgs& args, hipStream_t stream); \
+    inline hipError_t launch_scaled_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream) {   \
+        if (cfg_is_stream(cfg)) return launch_scaled_stream_##out(cfg, mode, inject, args, stream);                  \
+        if (cfg_is_generic(cfg)) return launch_scaled_generic_##out(cfg, mode, inject, args, stream);                \
+        return launch_scaled_fast_##out(cfg, mode, inject, args, stream);                                            \
+    }
+ABFT_DECLARE_SCALED(f16)
+ABFT_DECLARE_SCALED(bf16)
+#undef ABFT_DECLARE_SCALED
+
 }  // namespace abft

@@ -1,0 +1,6 @@
+// Generic kernel, int8 operands, results scaled to bf16.
+#define ABFT_DT abft::DT_I8
+#define ABFT_OUT abft::DT_BF16
+#define ABFT_FAMILY 3
+#define ABFT_LAUNCH_NAME launch_scaled_generic_bf16
+#include "gemm_launch.inc"

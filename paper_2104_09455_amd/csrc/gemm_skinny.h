@@ -29,7 +29,7 @@ constexpr int skinny_lds_bytes(int tn) { return SKINNY_WAVES * (1 + tn) * 2048; 
 // hook): in the sum of those of the eight shares that the tiling whose place this kernel takes has in one (p.n_parts shares, k tile t in
 // share t % p.n_parts), as it stands once that share has taken all its k tiles up to p.f_kt (-1: up to the last), or in the finished sum (-2).
 // The loop and the comparison are those of a call without one, and so is every other element.
-template <int DT, int TN, int MODE, bool BYTES, bool INJ>
+template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT>
 __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char* smem) {
     typedef Mma<DT, 16> MMA;
     typedef typename MMA::Acc Acc;
@@ -44,6 +44,18 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
     const int M = p.M, N = p.N, K = p.K, n0 = tile_n * 16 * TN;
     const int kb = K * ES, nkt = (kb + 127) >> 7;
     const int n_own = nkt > wave ? (nkt - wave + KW - 1) / KW : 0;
+
+    // scaled products (OUT: the 16-bit type they are stored in): the scales of what this wavefront stores at the end, on
+    // their way before the operands
+    constexpr bool SCALED = OUT != DT;
+    f32x4 row_scale;
+    float col_scale, col_bias;
+    if constexpr (SCALED) {
+        const int n = min(n0 + 16 * (TN == 1 ? 0 : wave & 1) + lrow, N - 1);
+        row_scale = row_scales(p, 4 * lgrp);
+        col_scale = p.col_scale[n];
+        col_bias = p.bias ? p.bias[n] : 0.f;
+    }
 
     // Copies: lane l takes chunk l % 8 of rows l / 8 and 8 + l / 8 of a k tile (whole lines; with a lane per row, as the
     // fragments want them, an instruction of 1 KB takes the vector memory path 64 clocks, so 17), writes them to its
@@ -207,11 +219,13 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 4 * lgrp + r;
-                const AccT o = p.act ? relu(v[r]) : v[r];
+                typename std::conditional<SCALED, float, AccT>::type o;
+                if constexpr (SCALED) o = scaled_value(v[r], row_scale[r], col_scale, col_bias, p.act);
+                else o = p.act ? relu(v[r]) : v[r];
                 if (row < M) {
-                    char* const dst = p.C + ((long long)row * p.ldc + col) * (IS_INT ? 4 : 2);
-                    if constexpr (DT == DT_F16) *reinterpret_cast<_Float16*>(dst) = (_Float16)o;
-                    else if constexpr (DT == DT_BF16) *reinterpret_cast<__bf16*>(dst) = (__bf16)o;
+                    char* const dst = p.C + ((long long)row * p.ldc + col) * (OUT == DT_I8 ? 4 : 2);
+                    if constexpr (OUT == DT_F16) *reinterpret_cast<_Float16*>(dst) = (_Float16)o;
+                    else if constexpr (OUT == DT_BF16) *reinterpret_cast<__bf16*>(dst) = (__bf16)o;
                     else *reinterpret_cast<int*>(dst) = o;
                 }
             }
@@ -274,12 +288,12 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
     }
 }
 
-template <int DT, int TN, int MODE, bool BYTES, bool INJ>
+template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT>
 __global__ __launch_bounds__(64 * SKINNY_WAVES) void gemm_skinny_kernel(const GemmArgs p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     int tile_m, tile_n;
     tile_of_block((int)blockIdx.x, 1, (int)gridDim.x, tile_m, tile_n);   // (a run of columns per die: whole lines of C and A once)
-    skinny_tile<DT, TN, MODE, BYTES, INJ>(p, tile_n, smem);
+    skinny_tile<DT, TN, MODE, BYTES, INJ, OUT>(p, tile_n, smem);
 }
 
 }  // namespace abft

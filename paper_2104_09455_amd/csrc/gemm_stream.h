@@ -131,6 +131,19 @@ __device__ __forceinline__ void stream_tile(const GemmArgs& p, int tile_m, int t
             else betaw_ptr = p.beta_p + blk * 8 + (2 + (lane >> 5)) * 2 * (long long)p.K + (long long)wave * BK * 2 + (lane & 31) * 4;
         }
     }
+    // scaled products: the scales of what this wavefront stores at the end, on their way before the operands
+    f32x4 row_scale[CFG::SCALED ? CFG::TM : 1];
+    float col_scale[CFG::SCALED ? CFG::TN : 1], col_bias[CFG::SCALED ? CFG::TN : 1];
+    if constexpr (CFG::SCALED) {
+#pragma unroll
+        for (int i = 0; i < CFG::TM; ++i) row_scale[i] = row_scales(p, bm0 + i * 32 + 8 * (wave & 3) + 4 * (lane >> 5));
+#pragma unroll
+        for (int j = 0; j < CFG::TN; ++j) {
+            const int n = min(bn0 + j * 32 + (lane & 31), N - 1);
+            col_scale[j] = p.col_scale[n];
+            col_bias[j] = p.bias ? p.bias[n] : 0.f;
+        }
+    }
     constexpr int BETA_ADV = KW * (MDOT ? 128 : BK * 4);
     // first k offset (within a k tile) of the four bytes this lane copies: one float, two halves of a
     // plane, or four digits of a plane
@@ -424,15 +437,20 @@ __device__ __forceinline__ void stream_tile(const GemmArgs& p, int tile_m, int t
                 }
             }
             // stored values: after the activation function; the checks below see the product
-            AccT o[4];
+            typename std::conditional<CFG::SCALED, float, AccT>::type o[4];
+            if constexpr (CFG::SCALED) {
 #pragma unroll
-            for (int rr = 0; rr < 4; ++rr) o[rr] = (p.act && !(v[rr] > 0)) ? (AccT)0 : v[rr];
+                for (int rr = 0; rr < 4; ++rr) o[rr] = scaled_value(v[rr], row_scale[i][rr], col_scale[j], col_bias[j], p.act);
+            } else {
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) o[rr] = (p.act && !(v[rr] > 0)) ? (AccT)0 : v[rr];
+            }
             if constexpr (CFG::CSIZE == 2) {
                 if (whole) {
                     // rows 8w + 4 (lane / 32) + 0..3 of this block, four columns per lane
                     char* dst = p.C + ((long long)(tc.bm0 + i * 32 + 8 * wave + 4 * tc.lgrp + (lane & 3)) * p.ldc +
                                        tc.bn0 + j * 32 + (tc.lrow & ~3)) * 2;
-                    store_quad_rows<DT>(o[0], o[1], o[2], o[3], dst, lane);
+                    store_quad_rows<CFG::OUT>(o[0], o[1], o[2], o[3], dst, lane);
                 }
             }
             if (CFG::CSIZE != 2 || !whole) {
@@ -441,8 +459,8 @@ __device__ __forceinline__ void stream_tile(const GemmArgs& p, int tile_m, int t
                     const int row = tc.bm0 + i * 32 + 8 * wave + 4 * tc.lgrp + rr;
                     if (row < M && col < N) {
                         char* dst = p.C + ((long long)row * p.ldc + col) * CFG::CSIZE;
-                        if constexpr (DT == DT_F16) *reinterpret_cast<_Float16*>(dst) = (_Float16)o[rr];
-                        else if constexpr (DT == DT_BF16) *reinterpret_cast<__bf16*>(dst) = (__bf16)o[rr];
+                        if constexpr (CFG::OUT == DT_F16) *reinterpret_cast<_Float16*>(dst) = (_Float16)o[rr];
+                        else if constexpr (CFG::OUT == DT_BF16) *reinterpret_cast<__bf16*>(dst) = (__bf16)o[rr];
                         else *reinterpret_cast<int*>(dst) = o[rr];
                     }
                 }
