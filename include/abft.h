@@ -6,7 +6,7 @@
  * the result with algorithm-based fault tolerance, following Kosaian & Rashmi,
  * "Arithmetic-Intensity-Guided Fault Tolerance for Neural Network Inference on
  * GPUs" (SC '21).  For language models it also holds what stands between such products when their
- * weights are int8: quantised linear layers and a paged cache of keys and values.  Notation is the paper's (Sec. 2.1): A is M x K (activations),
+ * weights are int8: quantised linear layers, a paged cache of keys and values, attention over it.  Notation is the paper's (Sec. 2.1): A is M x K (activations),
  * B is K x N (weights, known before inference), C is M x N.
  *
  * General conventions
@@ -471,11 +471,12 @@ int abft_linear_scaled(int M, int N, int K, const void *X, int64_t ldx, int dtyp
 /* Bytes of workspace abft_linear_scaled wants (0 for invalid arguments). */
 size_t abft_linear_scaled_workspace_bytes(int M, int N, int K, int mode);
 
-/* ---- a paged cache of keys and values ----------------------------------------- */
+/* ---- a paged cache of keys and values, and attention over it ------------------ */
 /* The cache of one attention layer: `pages` pages of `page_size` tokens.  A token's place is a slot,
  * page * page_size + its offset in the page; which pages a sequence has, in order, is the caller's block table.
- *   k, v            : pages x heads x page_size x head_dim, 16-byte aligned
- *   k_scale, v_scale: pages x heads x page_size floats; ABFT_I8 only, else NULL
+ *   k, v            : pages x heads x page_size x head_dim
+ *   k_scale, v_scale: pages x heads x page_size floats; ABFT_I8 only, else not looked at
+ *                     (all 16-byte aligned, else ABFT_E_LD)
  *   dtype           : ABFT_I8 (integers with a scale for each token and head, the rule of abft_quantize_rows over
  *                     head_dim values), or ABFT_F16 / ABFT_BF16 (the values as they are)
  *   page_size       : a multiple of 16 up to 4096 (ABFT_E_VALUE); pages * page_size below 2^31
@@ -500,6 +501,38 @@ int abft_kv_write(const abft_kv_cache_t *cache /* host */, int tokens, const int
  * zeros.  Layout, types and checks as for abft_kv_write. */
 int abft_kv_read(const abft_kv_cache_t *cache /* host */, int tokens, const int64_t *slots, void *K, int64_t ldk, void *V,
                  int64_t ldv, int dtype, void *stream);
+
+/* Attention of the newest tokens of n_seqs sequences over their cache (which already holds those tokens' keys and
+ * values): sequence s has the tokens q_start[s] .. q_start[s + 1] - 1 of the batch, the last ones of its kv_len[s] tokens
+ * in the cache.  Row (t, h) is query head h of the i-th of a sequence's nq new tokens, at position
+ * p = kv_len - nq + i; it sees the keys j of the sequence with
+ *     j < kv_len;   causal: j <= p;   window > 0: j > p - window
+ * and O[t][h] = sum_j w_j v_j / sum_j w_j, w_j = exp(scale * q . k_j - max), with the keys and values of head h / (q_heads /
+ * heads).  A row that sees nothing (kv_len 0, or more new tokens than the cache holds) is zero.  What a row does not see does
+ * not touch it, infinities and NaN included.
+ *   q_start: n_seqs + 1 int32 (device), ascending from 0 to total_q; kv_len: n_seqs int32 (device), 0 .. max_kv
+ *   block_table: int32 (device), row s the page numbers of sequence s, rows ld_table apart; ld_table * page_size >= max_kv.
+ *          Entries of pages that hold no token of the sequence are not used.
+ *   total_q, max_q, max_kv (host): all new tokens; upper bounds of a sequence's new tokens and of kv_len (both set how the
+ *          work is divided).  Device values beyond them are cut to them, and page numbers to the cache, so that nothing
+ *          outside the buffers is read; rows whose numbers were cut have unspecified values.  max_kv <= 2^24.
+ *   Q    : total_q rows of q_heads * head_dim values, ldq apart; F16 / BF16, 16-byte aligned rows (ABFT_E_LD, as for the
+ *          other leading dimensions); q_heads a multiple of cache.heads.  A 16-bit cache has the type of Q.
+ *   O    : the same shape, rows ldo apart, of the type of Q, 8-byte aligned rows.
+ *   scale: finite and above 0 (ABFT_E_VALUE).
+ *   workspace: abft_attention_workspace_bytes(...) bytes, 256-byte aligned; may be NULL when that is 0.
+ *          No initialisation; calls that share one must be ordered on one stream.
+ * The products run on the matrix unit in the type of Q (int8 keys and values are exact there), softmax statistics
+ * and sums in fp32; the weights w_j are rounded to the type of Q.  The scheme of this library's products does not extend to these
+ * two: they are not checked.  Results do not depend on the other sequences of the call, but for the split of long key ranges,
+ * which follows n_seqs, total_q, max_q and max_kv. */
+int abft_attention(const abft_kv_cache_t *cache /* host */, int n_seqs, const int32_t *q_start, const int32_t *kv_len,
+                   const int32_t *block_table, int64_t ld_table, int total_q, int max_q, int max_kv, const void *Q,
+                   int64_t ldq, int q_heads, int dtype, float scale, int causal, int window, void *O, int64_t ldo,
+                   void *workspace, size_t workspace_bytes, void *stream);
+/* Bytes of workspace abft_attention wants for these arguments (0: none, or arguments it refuses). */
+size_t abft_attention_workspace_bytes(const abft_kv_cache_t *cache /* host */, int n_seqs, int total_q, int max_q, int max_kv,
+                                      int q_heads, int dtype);
 
 /* ---- misc ------------------------------------------------------------------ */
 const char *abft_strerror(int code);

@@ -68,7 +68,7 @@ EXPORTS = [
     "abft_tolerance_half_coeff", "abft_plan_run_chain", "abft_plan_chain_status", "abft_plan_chain_reset",
     "abft_plan_set_diagnostics", "abft_kernel_name", "abft_handover_launches", "abft_chain_launches", "abft_shared_launches", "abft_mfma_probe", "abft_mfma_probe_bytes",
     "abft_quantize_rows", "abft_gemm_scaled", "abft_linear_scaled", "abft_linear_scaled_workspace_bytes",
-    "abft_kv_write", "abft_kv_read",
+    "abft_kv_write", "abft_kv_read", "abft_attention", "abft_attention_workspace_bytes",
 ]
 
 _lib = None
@@ -185,6 +185,10 @@ def lib() -> ctypes.CDLL:
     for f in (L.abft_kv_write, L.abft_kv_read):
         f.restype = ci
         f.argtypes = [cp, ci, vp, vp, i64, vp, i64, ci, vp]
+    L.abft_attention.restype = ci
+    L.abft_attention.argtypes = [cp, ci, vp, vp, vp, i64, ci, ci, ci, vp, i64, ci, ci, ctypes.c_float, ci, ci, vp, i64, vp, sz, vp]
+    L.abft_attention_workspace_bytes.restype = sz
+    L.abft_attention_workspace_bytes.argtypes = [cp, ci, ci, ci, ci, ci, ci]
     _lib = L
     return L
 
@@ -487,3 +491,14 @@ def abft_kv_write(cache: KVCache, tokens, slots, K, ldk, V, ldv, dtype, stream=N
 
 def abft_kv_read(cache: KVCache, tokens, slots, K, ldk, V, ldv, dtype, stream=None) -> None:
     _check(lib().abft_kv_read(ctypes.byref(cache), tokens, _ptr(slots), _ptr(K), ldk, _ptr(V), ldv, dtype, _stream(stream)))
+
+
+def abft_attention(cache: KVCache, n_seqs, q_start, kv_len, block_table, ld_table, total_q, max_q, max_kv, Q, ldq, q_heads, dtype,
+                   scale, causal, window, O, ldo, workspace=None, workspace_bytes=0, stream=None) -> None:
+    _check(lib().abft_attention(ctypes.byref(cache), n_seqs, _ptr(q_start), _ptr(kv_len), _ptr(block_table), ld_table, total_q, max_q,
+                                max_kv, _ptr(Q), ldq, q_heads, dtype, scale, int(causal), window, _ptr(O), ldo, _ptr(workspace),
+                                workspace_bytes, _stream(stream)))
+
+
+def abft_attention_workspace_bytes(cache: KVCache, n_seqs, total_q, max_q, max_kv, q_heads, dtype) -> int:
+    return lib().abft_attention_workspace_bytes(ctypes.byref(cache), n_seqs, total_q, max_q, max_kv, q_heads, dtype)

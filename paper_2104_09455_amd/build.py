@@ -26,7 +26,7 @@ FLAGS += os.environ.get("ABFT_EXTRA_HIPCC_FLAGS", "").split()   # e.g. -D switch
 SOURCES = [f"gemm_{family}_{dt}.hip" for family in ("fast", "generic", "stream", "group") for dt in ("f16", "bf16", "i8")]
 SOURCES += [f"gemm_scaled_{family}_{out}.hip" for family in ("generic", "fast", "stream") for out in ("f16", "bf16")]
 SOURCES += ["gemm_strip_f16.hip", "gemm_strip_bf16.hip", "abft_api.hip"] + [f"gemm_skinny_{dt}.hip" for dt in ("f16", "bf16", "i8")]
-SOURCES += ["gemm_scaled_skinny.hip", "kv_cache.hip"]
+SOURCES += ["gemm_scaled_skinny.hip", "kv_cache.hip", "attention_f16.hip", "attention_bf16.hip", "attention_api.hip"]
 
 
 def _compile(src: str) -> str:

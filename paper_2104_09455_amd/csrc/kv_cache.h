@@ -16,7 +16,9 @@ inline int kv_validate(const abft_kv_cache_t* c, int dtype) {
     if (c->page_size <= 0 || c->page_size % 16 != 0 || c->page_size > KV_MAX_PAGE) return ABFT_E_VALUE;
     if ((long long)c->pages * c->page_size > 0x7fffffffll) return ABFT_E_SHAPE;
     if (!c->k || !c->v || (c->dtype == ABFT_I8 && (!c->k_scale || !c->v_scale))) return ABFT_E_NULL;
-    if (((reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v)) & 15u) != 0) return ABFT_E_LD;
+    uintptr_t at = reinterpret_cast<uintptr_t>(c->k) | reinterpret_cast<uintptr_t>(c->v);
+    if (c->dtype == ABFT_I8) at |= reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale);
+    if ((at & 15u) != 0) return ABFT_E_LD;
     return ABFT_OK;
 }
 

@@ -79,7 +79,7 @@ def test_linear_workspace():
 
 
 CACHE = dict(k=P, v=P, k_scale=P, v_scale=P, dtype=B.I8, pages=4, page_size=16, heads=2, head_dim=64)
-BAD_CACHES = [(dict(k=None), E_NULL), (dict(v=None), E_NULL), (dict(k_scale=None), E_NULL), (dict(v_scale=None), E_NULL), (dict(k=P + 8), E_LD),
+BAD_CACHES = [(dict(k=None), E_NULL), (dict(v=None), E_NULL), (dict(k_scale=None), E_NULL), (dict(v_scale=None), E_NULL), (dict(k=P + 8), E_LD), (dict(v_scale=P + 4), E_LD),
               (dict(dtype=B.BF16), E_ENUM), (dict(dtype=5), E_ENUM), (dict(pages=0), E_SHAPE), (dict(heads=0), E_SHAPE), (dict(head_dim=24), E_SHAPE),
               (dict(head_dim=0), E_SHAPE), (dict(head_dim=144), E_SHAPE), (dict(page_size=0), E_VALUE), (dict(page_size=24), E_VALUE),
               (dict(page_size=8192), E_VALUE), (dict(pages=1 << 27), E_SHAPE)]
@@ -106,3 +106,24 @@ def test_bad_tokens(change, code, move):
 def test_no_cache():
     assert B.lib().abft_kv_write(None, 1, P, P, 128, P, 128, B.F16, None) == E_NULL
     assert B.lib().abft_kv_read(ctypes.POINTER(B.KVCache)(), 1, P, P, 128, P, 128, B.F16, None) == E_NULL
+
+
+@pytest.mark.parametrize("change,code", BAD_CACHES)
+def test_attention_over_bad_caches(change, code):
+    cache = B.kv_cache(**dict(CACHE, **change))
+    refuses(code, lambda: B.abft_attention(cache, 2, P, P, P, 4, 5, 4, 60, P, 128, 2, B.F16, 0.1, True, 0, P, 128, workspace=P, workspace_bytes=1 << 40, stream=0))
+    assert B.abft_attention_workspace_bytes(cache, 2, 5, 4, 60, 2, B.F16) == 0
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(n_seqs=0), E_SHAPE), (dict(total_q=-1), E_SHAPE), (dict(max_q=6), E_SHAPE), (dict(max_q=-1), E_SHAPE), (dict(max_kv=-1), E_SHAPE),
+    (dict(max_kv=(1 << 24) + 1), E_SHAPE), (dict(q_heads=0), E_SHAPE), (dict(q_heads=3), E_SHAPE), (dict(q_start=None), E_NULL), (dict(kv_len=None), E_NULL),
+    (dict(block_table=None), E_NULL), (dict(Q=None), E_NULL), (dict(O=None), E_NULL), (dict(dtype=B.I8), E_ENUM), (dict(scale=0.0), E_VALUE),
+    (dict(scale=float("nan")), E_VALUE), (dict(scale=float("inf")), E_VALUE), (dict(scale=-1.0), E_VALUE), (dict(window=-1), E_VALUE), (dict(ldq=255), E_LD),
+    (dict(ldo=255), E_LD), (dict(ldq=260), E_LD), (dict(ldo=258), E_LD), (dict(Q=P + 8), E_LD), (dict(O=P + 4), E_LD), (dict(ld_table=312), E_LD),
+    (dict(workspace=None), E_WORKSPACE), (dict(workspace=P + 64), E_WORKSPACE), (dict(workspace_bytes=100), E_WORKSPACE)])
+def test_attention(change, code):
+    a = dict(n_seqs=2, q_start=P, kv_len=P, block_table=P, ld_table=313, total_q=5, max_q=4, max_kv=5000, Q=P, ldq=256, q_heads=4, dtype=B.BF16, scale=0.1, causal=True,
+             window=0, O=P, ldo=256, workspace=P, workspace_bytes=1 << 40)
+    a.update(change)
+    refuses(code, lambda: B.abft_attention(B.kv_cache(**CACHE), stream=0, **a))
