@@ -5,11 +5,12 @@
 #include <cmath>
 #include <cstring>
 
-#include "attention.h"
+#include "attention_single.h"
+#include "attention_tile.h"
 
 namespace abft {
-hipError_t launch_attention_f16(const AttnArgs& a, bool i8, int tiles, long long join_rows, hipStream_t stream);
-hipError_t launch_attention_bf16(const AttnArgs& a, bool i8, int tiles, long long join_rows, hipStream_t stream);
+hipError_t launch_attention_f16(const AttnArgs& a, bool i8, int tiles, hipStream_t stream);
+hipError_t launch_attention_bf16(const AttnArgs& a, bool i8, int tiles, hipStream_t stream);
 }  // namespace abft
 
 using namespace abft;
@@ -20,14 +21,13 @@ long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr int MAX_KV = 1 << 24;
-constexpr int SINGLE_CHUNK_MAX = 4096;   // (a wavefront keeps the page numbers of its share in its lanes: 64 blocks of 16 keys)
+constexpr int COMPUTE_UNITS = 256;
 
 // How a call's work is divided, from what the host knows of it.
 struct Division {
-    int single, single_chunk, single_splits;
+    int single, single_groups;
     int tiles, tile_chunk, tile_splits;      // tiles: an upper bound of the row tiles, 0: none can be there
     size_t off_single_ml, off_tile_o, off_tile_ml, bytes;
-    long long join_rows;
 };
 Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max_kv, int q_heads) {
     Division d;
@@ -36,14 +36,13 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
     // sequences of one token have a kernel; where all have the same number of tokens, and more than one, there are none
     d.single = group <= ATTN_GROUP_MAX && (max_q == 1 || (long long)n * max_q != total_q);
     const bool tiled = !d.single || max_q > 1;
-    d.single_chunk = SINGLE_CHUNK_MAX;
-    d.single_splits = d.tile_splits = 1;
+    d.tile_splits = 1;
     d.tile_chunk = (int)(cdiv(std::max(max_kv, 1), ATTN_BLOCK_KEYS) * ATTN_BLOCK_KEYS);
     if (d.single) {
-        // four workgroups per compute unit, if the keys give that many pieces of 256
-        const long long keys = cdiv((long long)max_kv * n * c->heads, 1024);
-        d.single_chunk = (int)std::min<long long>(SINGLE_CHUNK_MAX, std::max<long long>(256, cdiv(keys, 128) * 128));
-        d.single_splits = (int)std::max<long long>(1, cdiv(max_kv, d.single_chunk));
+        // all workgroups that the chip holds, if the keys give four units for each
+        const long long units = cdiv(max_kv, SINGLE_UNIT) * n * c->heads;
+        const int most = COMPUTE_UNITS * single_per_cu(c->head_dim <= 64 ? 64 : 128);
+        d.single_groups = (int)std::min<long long>(most, std::max<long long>(std::min<long long>((long long)n * c->heads, most), cdiv(units, 4)));
     }
     if (tiled) {
         d.tiles = n + (int)((long long)total_q * group / AttnTile<128>::ROWS);
@@ -61,13 +60,12 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
         at = align_up(at + floats * 4, 256);
         return here;
     };
-    const size_t singles = d.single_splits > 1 ? (size_t)n * q_heads : 0, rows = d.tile_splits > 1 ? (size_t)total_q * q_heads : 0;
-    take(singles * d.single_splits * c->head_dim);
-    d.off_single_ml = take(singles * d.single_splits * 2);
-    d.off_tile_o = take(rows * d.tile_splits * c->head_dim);
-    d.off_tile_ml = take(rows * d.tile_splits * 2);
+    const size_t places = (size_t)2 * d.single_groups * group, rows = d.tile_splits > 1 ? (size_t)total_q * q_heads * d.tile_splits : 0;
+    take(places * c->head_dim);
+    d.off_single_ml = take(places * 2);
+    d.off_tile_o = take(rows * c->head_dim);
+    d.off_tile_ml = take(rows * 2);
     d.bytes = at;
-    d.join_rows = (long long)(singles + rows);
     return d;
 }
 
@@ -76,7 +74,7 @@ int validate(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max_kv
     if (rc != ABFT_OK) return rc;
     if (n <= 0 || total_q < 0 || max_q < 0 || max_q > total_q || max_kv < 0 || max_kv > MAX_KV) return ABFT_E_SHAPE;
     if (q_heads <= 0 || q_heads % c->heads != 0) return ABFT_E_SHAPE;
-    if ((long long)total_q * q_heads > 0x7fffffffll || (long long)n * q_heads * std::max(1, max_kv / 256) > 0x7fffffffll) return ABFT_E_SHAPE;
+    if ((long long)total_q * q_heads > 0x7fffffffll || (long long)n * q_heads * (max_kv / SINGLE_UNIT + 1) > 0x7fffffffll) return ABFT_E_SHAPE;
     return ABFT_OK;
 }
 
@@ -109,7 +107,7 @@ int abft_attention(const abft_kv_cache_t* cache, int n_seqs, const int32_t* q_st
     a.ks = cache->k_scale; a.vs = cache->v_scale;
     a.pages = cache->pages; a.page_size = cache->page_size; a.heads = cache->heads; a.dim = cache->head_dim;
     a.page_blocks = (unsigned)cache->page_size / 16;
-    a.page_magic = a.page_blocks > 1 ? (unsigned)cdiv(1ll << 32, a.page_blocks) : 0;
+    a.page_magic = (unsigned)cdiv(1ll << 31, a.page_blocks);
     a.q_start = q_start; a.kv_len = kv_len; a.table = block_table; a.ld_table = ld_table;
     a.n_seqs = n_seqs; a.total_q = total_q; a.max_q = max_q; a.max_kv = max_kv;
     a.Q = reinterpret_cast<const char*>(Q); a.O = reinterpret_cast<char*>(O); a.ldq = ldq; a.ldo = ldo;
@@ -117,10 +115,10 @@ int abft_attention(const abft_kv_cache_t* cache, int n_seqs, const int32_t* q_st
     a.c = scale * 1.44269504f;
     a.causal = causal != 0; a.window = window;
     a.single = d.single;
-    a.single_chunk = d.single_chunk; a.single_splits = d.single_splits; a.tile_chunk = d.tile_chunk; a.tile_splits = d.tile_splits;
+    a.single_groups = d.single_groups; a.tile_chunk = d.tile_chunk; a.tile_splits = d.tile_splits;
     a.single_o = reinterpret_cast<float*>(ws); a.single_ml = reinterpret_cast<float*>(ws + d.off_single_ml);
     a.tile_o = reinterpret_cast<float*>(ws + d.off_tile_o); a.tile_ml = reinterpret_cast<float*>(ws + d.off_tile_ml);
-    const hipError_t e = (dtype == ABFT_F16 ? launch_attention_f16 : launch_attention_bf16)(a, cache->dtype == ABFT_I8, d.tiles, d.join_rows,
+    const hipError_t e = (dtype == ABFT_F16 ? launch_attention_f16 : launch_attention_bf16)(a, cache->dtype == ABFT_I8, d.tiles,
                                                                                            reinterpret_cast<hipStream_t>(stream));
     return e == hipSuccess ? ABFT_OK : ABFT_E_HIP;
 }
