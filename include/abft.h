@@ -520,8 +520,9 @@ int abft_kv_read(const abft_kv_cache_t *cache /* host */, int tokens, const int6
  *          other leading dimensions); q_heads a multiple of cache.heads.  A 16-bit cache has the type of Q.
  *   O    : the same shape, rows ldo apart, of the type of Q, 8-byte aligned rows.
  *   scale: finite and above 0 (ABFT_E_VALUE).
- *   workspace: abft_attention_workspace_bytes(...) bytes, 256-byte aligned; may be NULL when that is 0.
- *          No initialisation; calls that share one must be ordered on one stream.
+ *   workspace: abft_attention_workspace_bytes(...) bytes, 256-byte aligned; may be NULL when that is 0.  Its first 4096
+ *          bytes have to be zero before its first use, and are zero again after every call (of whatever shape); the rest needs
+ *          no initialisation.  Calls that share one must be ordered on one stream.
  * The products run on the matrix unit in the type of Q (int8 keys and values are exact there), softmax statistics
  * and sums in fp32; the weights w_j are rounded to the type of Q.  The scheme of this library's products does not extend to these
  * two: they are not checked.  Results do not depend on the other sequences of the call, but for the split of long key ranges,

@@ -40,6 +40,7 @@ struct AttnArgs {
     // Sequences of one new token have a kernel of their own (single: they are left to it): `single_groups` workgroups, and two
     // places each for sums of keys that are not all of a row's: group rows of dim floats, and of two (m, the sum of weights).
     int single, single_groups;
+    unsigned* counters;                 // one for each of them, zero before and after a launch
     float *single_o, *single_ml;
     // The others: tile_splits pieces of tile_chunk keys, and their sums, rows x splits of the same.
     int tile_chunk, tile_splits;

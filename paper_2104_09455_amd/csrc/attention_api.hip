@@ -21,13 +21,13 @@ long long cdiv(long long a, long long b) { return (a + b - 1) / b; }
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr int MAX_KV = 1 << 24;
-constexpr int COMPUTE_UNITS = 256;
+constexpr int COMPUTE_UNITS = 256, COUNTERS = COMPUTE_UNITS * 4;
 
 // How a call's work is divided, from what the host knows of it.
 struct Division {
     int single, single_groups;
     int tiles, tile_chunk, tile_splits;      // tiles: an upper bound of the row tiles, 0: none can be there
-    size_t off_single_ml, off_tile_o, off_tile_ml, bytes;
+    size_t off_single_o, off_single_ml, off_tile_o, off_tile_ml, bytes;
 };
 Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max_kv, int q_heads) {
     Division d;
@@ -61,7 +61,10 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
         return here;
     };
     const size_t places = (size_t)2 * d.single_groups * group, rows = d.tile_splits > 1 ? (size_t)total_q * q_heads * d.tile_splits : 0;
-    take(places * c->head_dim);
+    if (places + rows == 0) return d;
+    // (the counters first, always of one size: calls of different shapes share a workspace)
+    take(COUNTERS);
+    d.off_single_o = take(places * c->head_dim);
     d.off_single_ml = take(places * 2);
     d.off_tile_o = take(rows * c->head_dim);
     d.off_tile_ml = take(rows * 2);
@@ -116,7 +119,8 @@ int abft_attention(const abft_kv_cache_t* cache, int n_seqs, const int32_t* q_st
     a.causal = causal != 0; a.window = window;
     a.single = d.single;
     a.single_groups = d.single_groups; a.tile_chunk = d.tile_chunk; a.tile_splits = d.tile_splits;
-    a.single_o = reinterpret_cast<float*>(ws); a.single_ml = reinterpret_cast<float*>(ws + d.off_single_ml);
+    a.counters = reinterpret_cast<unsigned*>(ws);
+    a.single_o = reinterpret_cast<float*>(ws + d.off_single_o); a.single_ml = reinterpret_cast<float*>(ws + d.off_single_ml);
     a.tile_o = reinterpret_cast<float*>(ws + d.off_tile_o); a.tile_ml = reinterpret_cast<float*>(ws + d.off_tile_ml);
     const hipError_t e = (dtype == ABFT_F16 ? launch_attention_f16 : launch_attention_bf16)(a, cache->dtype == ABFT_I8, d.tiles,
                                                                                            reinterpret_cast<hipStream_t>(stream));

@@ -15,9 +15,8 @@ constexpr int single_per_cu(int dp) { return dp == 64 ? 4 : 3; }   // workgroups
 // the first key that a single token sees (it is the last one itself), and its units: one at least, since its rows have to be written
 __device__ __forceinline__ int single_lo(const AttnArgs& p, int kv) { return p.window > 0 ? max(kv - p.window, 0) : 0; }
 __device__ __forceinline__ unsigned single_units(const AttnArgs& p, const SeqInfo& i) {
-    if (i.nq != 1) return 0;
     const int from = single_lo(p, i.kv) & ~(SINGLE_UNIT - 1);
-    return (unsigned)max(1, (i.kv - from + SINGLE_UNIT - 1) / SINGLE_UNIT);
+    return i.nq == 1 ? (unsigned)max(1, (i.kv - from + SINGLE_UNIT - 1) / SINGLE_UNIT) : 0;
 }
 
 // How the units of a launch are dealt: workgroup b has units first(b) to first(b + 1) - 1.
@@ -29,14 +28,22 @@ struct Shares {
         return u < big ? u / (per + 1) : more + (u - big) / max(per, 1u);
     }
 };
-// A wavefront's look at the launch: the shares, and, with seq < 0, the sequence that holds workgroup b's first unit (-1: it has none),
-// else that sequence; and the sequence's first unit.
-__device__ __forceinline__ Shares single_plan(const AttnArgs& p, unsigned b, int& seq, unsigned& seq_first) {
+// A wavefront's look at the launch: the shares, the sequence that holds workgroup b's first unit (seq; -1: it has none), what is known of
+// it, and its own first unit.
+struct SingleStart {
+    Shares sh;
+    SeqInfo si;
+    int seq;
+    unsigned seq_first;
+};
+__device__ __forceinline__ SingleStart single_start(const AttnArgs& p, unsigned b) {
     const int lane = threadIdx.x & 63;
-    // units of 64 sequences, and the sums up to each of them
+    // 64 sequences: what is known of them, their units, and the sums up to each of them
+    SeqInfo i;
     unsigned n, sum;
     auto look = [&](int s0) {
-        n = s0 + lane < p.n_seqs ? single_units(p, seq_info(p, s0 + lane)) * (unsigned)p.heads : 0;
+        i = seq_info(p, min(s0 + lane, p.n_seqs - 1));   // (three loads without a condition)
+        n = s0 + lane < p.n_seqs ? single_units(p, i) * (unsigned)p.heads : 0;
         sum = n;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -49,24 +56,44 @@ __device__ __forceinline__ Shares single_plan(const AttnArgs& p, unsigned b, int
         look(s0);
         total += readlane(sum, 63);
     }
-    Shares sh;
-    sh.per = total / (unsigned)p.single_groups;
-    sh.more = total - sh.per * (unsigned)p.single_groups;
-    const unsigned unit = sh.first(b);
+    SingleStart st;
+    st.sh.per = total / (unsigned)p.single_groups;
+    st.sh.more = total - st.sh.per * (unsigned)p.single_groups;
+    st.seq = -1;
+    const unsigned unit = st.sh.first(b);
     unsigned before = 0;
-    int found = -1;
-    for (int s0 = 0; s0 < p.n_seqs && found < 0; s0 += 64) {
+    for (int s0 = 0; s0 < p.n_seqs && st.seq < 0; s0 += 64) {
         if (p.n_seqs > 64) look(s0);   // (else it has been)
-        const unsigned long long at = __ballot(seq < 0 ? before + sum > unit : s0 + lane == seq);
+        const unsigned long long at = __ballot(before + sum > unit);
         if (at != 0) {
             const int l = __builtin_ctzll(at);
-            found = s0 + l;
-            seq_first = before + readlane(sum, l) - readlane(n, l);
+            st.seq = s0 + l;
+            st.si.q0 = readlane(i.q0, l);
+            st.si.nq = readlane(i.nq, l);
+            st.si.kv = readlane(i.kv, l);
+            st.seq_first = before + readlane(sum, l) - readlane(n, l);
         }
         before += readlane(sum, 63);
     }
-    seq = found;
-    return sh;
+    return st;
+}
+
+// two floats that workgroups on other dies read in the same launch, and read so
+__device__ __forceinline__ void put_shared(float* p, float a, float b) {
+    const unsigned long long v = (unsigned long long)bitcast<unsigned>(b) << 32 | bitcast<unsigned>(a);
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_shared(const float* p) {
+    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return float2{bitcast<float>((unsigned)v), bitcast<float>((unsigned)(v >> 32))};
+}
+// VD values of a row from d0 on, divided by the sum of weights
+template <int DT, int VD>
+__device__ __forceinline__ void single_store(const AttnArgs& p, int token, int qh, int d0, const float (&acc)[VD], float norm) {
+    char* const dst = p.O + (token * p.ldo + (long long)qh * p.dim + d0) * 2;
+#pragma unroll
+    for (int j = 0; j < VD; j += 4)
+        *reinterpret_cast<i32x2*>(dst + 2 * j) = i32x2{pack_out16<DT>(acc[j] * norm, acc[j + 1] * norm), pack_out16<DT>(acc[j + 2] * norm, acc[j + 3] * norm)};
 }
 
 template <int DT, bool I8, int DP>
@@ -79,14 +106,15 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
     typedef int Piece __attribute__((ext_vector_type(VW)));
     __shared__ __attribute__((aligned(16))) float out_o[4][16][DP];
     __shared__ float out_m[4][16], out_l[4][16];
+    __shared__ bool last_owner;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int bid = blockIdx.x;
-    int seq = -1;
-    unsigned seq_first = 0;
-    const Shares sh = single_plan(p, bid, seq, seq_first);
-    unsigned unit = sh.first(bid);
+    const SingleStart start = single_start(p, bid);
+    const Shares sh = start.sh;
+    int seq = start.seq;
+    unsigned unit = sh.first(bid), seq_first = start.seq_first;
     const unsigned share = unit, unit_end = sh.first(bid + 1);
     if (seq < 0 || unit >= unit_end) return;
 
@@ -104,7 +132,7 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
     for (int e = 0; e < 4; ++e) v_off[e] = (unsigned)((4 * g + e) * row_bytes + (col * VD < p.dim ? col * VD * ES : 0));
 
     // ---- the share, one head of a sequence after the other
-    SeqInfo si = seq_info(p, seq);
+    SeqInfo si = start.si;
     unsigned units = single_units(p, si);
     while (unit < unit_end) {
         while (unit >= seq_first + units * p.heads) {   // (sequences of other lengths have no units)
@@ -120,6 +148,7 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
         const int n_tiles = c_to > from ? (c_to - from + 31) >> 5 : 0;
         const int n_own = n_tiles > wave ? (n_tiles - wave + 3) >> 2 : 0;
         const bool first_here = unit == share, whole = unit == pair_first && here_end == pair_end;
+        const unsigned owner0 = whole ? bid : sh.owner(pair_first), owners = whole ? 1 : sh.owner(pair_end - 1) - owner0 + 1;
         unit = here_end;
 
         // the page numbers of own tile i's two blocks of sixteen keys, through the scalar cache, and the blocks' first keys as
@@ -319,44 +348,87 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
             }
             if (whole) {
                 const float norm = L == 0.f ? 0.f : 1.f / L;
-                char* const dst = p.O + (si.q0 * p.ldo + (long long)(head * p.group + row) * p.dim + d0) * 2;
-#pragma unroll
-                for (int j = 0; j < VD; j += 4)
-                    *reinterpret_cast<i32x2*>(dst + 2 * j) = i32x2{pack_out16<DT>(acc[j] * norm, acc[j + 1] * norm), pack_out16<DT>(acc[j + 2] * norm, acc[j + 3] * norm)};
+                single_store<DT, VD>(p, si.q0, head * p.group + row, d0, acc, norm);
             } else {
                 // a share's first head has its first place, its last the second: between them all are whole
                 const int place_row = (2 * bid + (first_here ? 0 : 1)) * p.group + row;
 #pragma unroll
-                for (int j = 0; j < VD; j += 4)
-                    *reinterpret_cast<f32x4*>(p.single_o + (long long)place_row * p.dim + d0 + j) = f32x4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
-                if (d0 == 0) {
-                    p.single_ml[2 * place_row] = M;
-                    p.single_ml[2 * place_row + 1] = L;
+                for (int j = 0; j < VD; j += 2) put_shared(p.single_o + (long long)place_row * p.dim + d0 + j, acc[j], acc[j + 1]);
+                if (d0 == 0) put_shared(p.single_ml + 2 * place_row, M, L);
+            }
+        }
+        if (!whole) {
+            // ---- whoever is the last of a head's owners puts their sums together.  (The counter is that of the first owner, of whose heads
+            // only the last can go on behind its share; it is back at zero when the launch ends.  The sums are written through to where
+            // every die reads them, and waited for, before the counter moves; fences in their place, which write back and drop a die's
+            // whole L2, took the 64 sequences from 108 to 162 us.)
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tid == 0) last_owner = __hip_atomic_fetch_add(p.counters + owner0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == owners - 1;
+            __syncthreads();
+            if (last_owner) {
+                if (tid == 0) __hip_atomic_store(p.counters + owner0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                // the first owner's place is its first only where its share starts with this head, the others' is their first
+                const int at0 = 2 * owner0 + (sh.first(owner0) == pair_first ? 0 : 1);
+                // sixteen threads a row, and as many such sets as there are: each takes every set-th owner
+                const int sets = 16 / p.group, set = row / p.group, r = row - set * p.group;
+                auto place_of = [&](unsigned i) { return (i == 0 ? at0 : 2 * (int)(owner0 + i)) * p.group + r; };
+                if (set < sets) {
+                    float M = ATTN_NONE;
+                    for (unsigned i = set + sets * (tid & 15); i < owners; i += 16 * sets) M = __builtin_fmaxf(M, get_shared(p.single_ml + 2 * place_of(i)).x);
+#pragma unroll
+                    for (int d = 1; d < 16; d <<= 1) M = __builtin_fmaxf(M, __shfl_xor(M, d));
+                    float L = 0.f, acc[VD];
+#pragma unroll
+                    for (int j = 0; j < VD; ++j) acc[j] = 0.f;
+                    const int d = d0 < p.dim ? d0 : 0;
+                    // four owners' sums on their way at a time
+                    for (unsigned i0 = set; i0 < owners; i0 += 4 * sets) {
+                        float2 ml[4], x[4][VD / 2];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int at = place_of(min(i0 + u * sets, owners - 1));
+                            ml[u] = get_shared(p.single_ml + 2 * at);
+#pragma unroll
+                            for (int j = 0; j < VD / 2; ++j) x[u][j] = get_shared(p.single_o + (long long)at * p.dim + d + 2 * j);
+                        }
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            if (i0 + u * sets >= owners) continue;
+                            const float f = __builtin_amdgcn_exp2f(ml[u].x - M);
+                            L = __builtin_fmaf(f, ml[u].y, L);
+#pragma unroll
+                            for (int j = 0; j < VD / 2; ++j) {
+                                acc[2 * j] = __builtin_fmaf(f, x[u][j].x, acc[2 * j]);
+                                acc[2 * j + 1] = __builtin_fmaf(f, x[u][j].y, acc[2 * j + 1]);
+                            }
+                        }
+                    }
+                    if ((tid & 15) == 0) {
+                        out_m[0][row] = M;
+                        out_l[0][row] = L;
+                    }
+#pragma unroll
+                    for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(&out_o[0][row][d0 + j]) = f32x4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
+                }
+                __syncthreads();
+                if (row < p.group && d0 < p.dim) {
+                    float M = ATTN_NONE, L = 0.f, acc[VD];
+                    for (int i = 0; i < sets; ++i) M = __builtin_fmaxf(M, out_m[0][i * p.group + row]);
+#pragma unroll
+                    for (int j = 0; j < VD; ++j) acc[j] = 0.f;
+                    for (int i = 0; i < sets; ++i) {
+                        const float f = __builtin_amdgcn_exp2f(out_m[0][i * p.group + row] - M);
+                        L = __builtin_fmaf(f, out_l[0][i * p.group + row], L);
+#pragma unroll
+                        for (int j = 0; j < VD; ++j) acc[j] = __builtin_fmaf(f, out_o[0][i * p.group + row][d0 + j], acc[j]);
+                    }
+                    single_store<DT, VD>(p, si.q0, head * p.group + row, d0, acc, L == 0.f ? 0.f : 1.f / L);
                 }
             }
         }
         __syncthreads();   // (the LDS is the next head's)
     }
-}
-
-// The sums of heads whose keys several workgroups shared, a wavefront per row.
-template <int DT>
-__global__ __launch_bounds__(256) void attn_single_join_kernel(const AttnArgs p) {
-    const int qheads = p.heads * p.group;
-    const long long row = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    int seq = (int)(row / qheads);
-    if (seq >= p.n_seqs) return;
-    const SeqInfo si = seq_info(p, seq);
-    if (si.nq != 1) return;
-    const int qh = (int)(row - (long long)seq * qheads), head = qh / p.group, r = qh - head * p.group;
-    unsigned seq_first = 0;
-    const Shares sh = single_plan(p, 0, seq, seq_first);
-    const unsigned units = single_units(p, si), u0 = seq_first + head * units;
-    const unsigned b0 = sh.owner(u0), b1 = sh.owner(u0 + units - 1);
-    if (b0 == b1) return;
-    // the first owner's place is its first only where its share starts with this head, the others' is their first
-    const unsigned at0 = sh.first(b0) == u0 ? 2 * b0 : 2 * b0 + 1;
-    attn_join_row<DT>(p, b1 - b0 + 1, [&](int i) { return (long long)(i == 0 ? at0 : 2 * (b0 + i)) * p.group + r; }, p.single_o, p.single_ml, si.q0, qh);
 }
 
 }  // namespace abft

@@ -72,10 +72,12 @@ class Case:
         out = torch.full((self.total + 1, ldo), 7.0, dtype=self.t, device=DEV)
         n = B.abft_attention_workspace_bytes(self.handle, len(self.q), self.total, max_q, max_kv, self.hq, self.dt)
         ws = torch.full((n,), 255, dtype=torch.uint8, device=DEV)   # (NaN)
+        ws[:4096] = 0
         torch.cuda.synchronize()
         B.abft_attention(self.handle, len(self.q), self.q_start, self.kv_len, self.table, self.width, self.total, max_q, max_kv, self.Q, self.ldq,
                          self.hq, self.dt, self.scale, self.causal, self.window, out, ldo, workspace=ws if n else None, workspace_bytes=n, stream=stream)
         torch.cuda.synchronize()
+        assert not ws[:4096].any()
         assert (out[:, self.hq * self.dim:] == 7.0).all() and (out[self.total] == 7.0).all()
         return out[:self.total, :self.hq * self.dim].reshape(self.total, self.hq, self.dim)
 
@@ -278,7 +280,7 @@ def test_attention_in_a_graph():
     c = Case([1] * 6, [900, 3, 2000, 64, 65, 1], 2, 4, 64, 16, "f16", "i8", seed=6, poison=False)
     out = torch.empty(c.total, c.hq, c.dim, dtype=c.t, device=DEV)
     n = B.abft_attention_workspace_bytes(c.handle, 6, 6, 1, 2000, c.hq, c.dt)
-    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    ws = torch.zeros(n, dtype=torch.uint8, device=DEV)
 
     def call():
         B.abft_attention(c.handle, 6, c.q_start, c.kv_len, c.table, c.width, 6, 1, 2000, c.Q, c.ldq, c.hq, c.dt, c.scale, True, 0, out, c.hq * c.dim,
