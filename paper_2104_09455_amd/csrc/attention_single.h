@@ -78,6 +78,12 @@ __device__ __forceinline__ SingleStart single_start(const AttnArgs& p, unsigned 
     return st;
 }
 
+// A head whose keys several workgroups share: its owners are owner0 and the ones behind it, whose sums lie at place0 (the first's)
+// and at their first places.
+struct Joint {
+    unsigned owner0, owners, place0;
+    int token, head;
+};
 // two floats that workgroups on other dies read in the same launch, and read so
 __device__ __forceinline__ void put_shared(float* p, float a, float b) {
     const unsigned long long v = (unsigned long long)bitcast<unsigned>(b) << 32 | bitcast<unsigned>(a);
@@ -106,7 +112,7 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
     typedef int Piece __attribute__((ext_vector_type(VW)));
     __shared__ __attribute__((aligned(16))) float out_o[4][16][DP];
     __shared__ float out_m[4][16], out_l[4][16];
-    __shared__ bool last_owner;
+    __shared__ bool last_owner[2];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -134,6 +140,7 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
     // ---- the share, one head of a sequence after the other
     SeqInfo si = start.si;
     unsigned units = single_units(p, si);
+    Joint head0 = {0, 0, 0, 0, 0}, head1 = {0, 0, 0, 0, 0};   // the heads that this share holds a part of: its first, its last
     while (unit < unit_end) {
         while (unit >= seq_first + units * p.heads) {   // (sequences of other lengths have no units)
             seq_first += units * p.heads;
@@ -148,7 +155,17 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
         const int n_tiles = c_to > from ? (c_to - from + 31) >> 5 : 0;
         const int n_own = n_tiles > wave ? (n_tiles - wave + 3) >> 2 : 0;
         const bool first_here = unit == share, whole = unit == pair_first && here_end == pair_end;
-        const unsigned owner0 = whole ? bid : sh.owner(pair_first), owners = whole ? 1 : sh.owner(pair_end - 1) - owner0 + 1;
+        if (!whole) {
+            // (the first owner's place is its first only where its share starts with this head, the others' is their first)
+            Joint j;
+            j.owner0 = sh.owner(pair_first);
+            j.owners = sh.owner(pair_end - 1) - j.owner0 + 1;
+            j.place0 = 2 * j.owner0 + (sh.first(j.owner0) == pair_first ? 0 : 1);
+            j.token = si.q0;
+            j.head = head;
+            if (first_here) head0 = j;
+            else head1 = j;
+        }
         unit = here_end;
 
         // the page numbers of own tile i's two blocks of sixteen keys, through the scalar cache, and the blocks' first keys as
@@ -357,77 +374,84 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
                 if (d0 == 0) put_shared(p.single_ml + 2 * place_row, M, L);
             }
         }
-        if (!whole) {
-            // ---- whoever is the last of a head's owners puts their sums together.  (The counter is that of the first owner, of whose heads
-            // only the last can go on behind its share; it is back at zero when the launch ends.  The sums are written through to where
-            // every die reads them, and waited for, before the counter moves; fences in their place, which write back and drop a die's
-            // whole L2, took the 64 sequences from 108 to 162 us.)
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-            if (tid == 0) last_owner = __hip_atomic_fetch_add(p.counters + owner0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == owners - 1;
-            __syncthreads();
-            if (last_owner) {
-                if (tid == 0) __hip_atomic_store(p.counters + owner0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                // the first owner's place is its first only where its share starts with this head, the others' is their first
-                const int at0 = 2 * owner0 + (sh.first(owner0) == pair_first ? 0 : 1);
-                // sixteen threads a row, and as many such sets as there are: each takes every set-th owner
-                const int sets = 16 / p.group, set = row / p.group, r = row - set * p.group;
-                auto place_of = [&](unsigned i) { return (i == 0 ? at0 : 2 * (int)(owner0 + i)) * p.group + r; };
-                if (set < sets) {
-                    float M = ATTN_NONE;
-                    for (unsigned i = set + sets * (tid & 15); i < owners; i += 16 * sets) M = __builtin_fmaxf(M, get_shared(p.single_ml + 2 * place_of(i)).x);
+        __syncthreads();   // (the LDS is the next head's)
+    }
+
+    // ---- whoever is the last of a head's owners puts their sums together.  (The counter is that of the first owner, of whose heads
+    // only the last can go on behind its share; it is back at zero when the launch ends.  The sums are written through to where
+    // every die reads them, and waited for, before the counter moves; fences in their place, which write back and drop a die's
+    // whole L2, took 64 sequences from 108 to 162 us.)
+    if (head0.owners + head1.owners == 0) return;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (lane == 0 && wave < 2) {
+        const unsigned owner0 = wave == 0 ? head0.owner0 : head1.owner0, owners = wave == 0 ? head0.owners : head1.owners;
+        last_owner[wave] = owners != 0 && __hip_atomic_fetch_add(p.counters + owner0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == owners - 1;
+    }
+    __syncthreads();
+    // sixteen threads a row, and as many such sets as there are: each takes every set-th owner
+    const int row = tid >> 4, d0 = (tid & 15) * VD, sets = 16 / p.group, set = row / p.group, r = row - set * p.group;
+    for (int which = 0; which < 2; ++which) {
+        if (!last_owner[which]) continue;
+        const Joint j = which == 0 ? head0 : head1;
+        if (tid == 0) __hip_atomic_store(p.counters + j.owner0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        auto place_of = [&](unsigned i) { return (int)(i == 0 ? j.place0 : 2 * (j.owner0 + i)) * p.group + r; };
+        float M = ATTN_NONE, L = 0.f, acc[VD];
 #pragma unroll
-                    for (int d = 1; d < 16; d <<= 1) M = __builtin_fmaxf(M, __shfl_xor(M, d));
-                    float L = 0.f, acc[VD];
+        for (int c = 0; c < VD; ++c) acc[c] = 0.f;
+        if (set < sets) {
+            const int d = d0 < p.dim ? d0 : 0;
+            // four owners' sums on their way at a time
+            for (unsigned i0 = set; i0 < j.owners; i0 += 4 * sets) {
+                float2 ml[4], x[4][VD / 2];
 #pragma unroll
-                    for (int j = 0; j < VD; ++j) acc[j] = 0.f;
-                    const int d = d0 < p.dim ? d0 : 0;
-                    // four owners' sums on their way at a time
-                    for (unsigned i0 = set; i0 < owners; i0 += 4 * sets) {
-                        float2 ml[4], x[4][VD / 2];
+                for (int u = 0; u < 4; ++u) {
+                    const int at = place_of(min(i0 + u * sets, j.owners - 1));
+                    ml[u] = get_shared(p.single_ml + 2 * at);
 #pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            const int at = place_of(min(i0 + u * sets, owners - 1));
-                            ml[u] = get_shared(p.single_ml + 2 * at);
-#pragma unroll
-                            for (int j = 0; j < VD / 2; ++j) x[u][j] = get_shared(p.single_o + (long long)at * p.dim + d + 2 * j);
-                        }
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            if (i0 + u * sets >= owners) continue;
-                            const float f = __builtin_amdgcn_exp2f(ml[u].x - M);
-                            L = __builtin_fmaf(f, ml[u].y, L);
-#pragma unroll
-                            for (int j = 0; j < VD / 2; ++j) {
-                                acc[2 * j] = __builtin_fmaf(f, x[u][j].x, acc[2 * j]);
-                                acc[2 * j + 1] = __builtin_fmaf(f, x[u][j].y, acc[2 * j + 1]);
-                            }
-                        }
-                    }
-                    if ((tid & 15) == 0) {
-                        out_m[0][row] = M;
-                        out_l[0][row] = L;
-                    }
-#pragma unroll
-                    for (int j = 0; j < VD; j += 4) *reinterpret_cast<f32x4*>(&out_o[0][row][d0 + j]) = f32x4{acc[j], acc[j + 1], acc[j + 2], acc[j + 3]};
+                    for (int c = 0; c < VD / 2; ++c) x[u][c] = get_shared(p.single_o + (long long)at * p.dim + d + 2 * c);
                 }
-                __syncthreads();
-                if (row < p.group && d0 < p.dim) {
-                    float M = ATTN_NONE, L = 0.f, acc[VD];
-                    for (int i = 0; i < sets; ++i) M = __builtin_fmaxf(M, out_m[0][i * p.group + row]);
+                // (the last owner more than once is no harm to a maximum)
+                const float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(ml[0].x, ml[1].x), __builtin_fmaxf(ml[2].x, ml[3].x)), M);
+                const float f0 = __builtin_amdgcn_exp2f(M - top);
+                M = top;
+                L *= f0;
 #pragma unroll
-                    for (int j = 0; j < VD; ++j) acc[j] = 0.f;
-                    for (int i = 0; i < sets; ++i) {
-                        const float f = __builtin_amdgcn_exp2f(out_m[0][i * p.group + row] - M);
-                        L = __builtin_fmaf(f, out_l[0][i * p.group + row], L);
+                for (int c = 0; c < VD; ++c) acc[c] *= f0;
 #pragma unroll
-                        for (int j = 0; j < VD; ++j) acc[j] = __builtin_fmaf(f, out_o[0][i * p.group + row][d0 + j], acc[j]);
+                for (int u = 0; u < 4; ++u) {
+                    if (i0 + u * sets >= j.owners) continue;
+                    const float f = __builtin_amdgcn_exp2f(ml[u].x - M);
+                    L = __builtin_fmaf(f, ml[u].y, L);
+#pragma unroll
+                    for (int c = 0; c < VD / 2; ++c) {
+                        acc[2 * c] = __builtin_fmaf(f, x[u][c].x, acc[2 * c]);
+                        acc[2 * c + 1] = __builtin_fmaf(f, x[u][c].y, acc[2 * c + 1]);
                     }
-                    single_store<DT, VD>(p, si.q0, head * p.group + row, d0, acc, L == 0.f ? 0.f : 1.f / L);
                 }
             }
+            if ((tid & 15) == 0) {
+                out_m[0][row] = M;
+                out_l[0][row] = L;
+            }
+#pragma unroll
+            for (int c = 0; c < VD; c += 4) *reinterpret_cast<f32x4*>(&out_o[0][row][d0 + c]) = f32x4{acc[c], acc[c + 1], acc[c + 2], acc[c + 3]};
         }
-        __syncthreads();   // (the LDS is the next head's)
+        __syncthreads();
+        if (row < p.group && d0 < p.dim) {
+            for (int i = 1; i < sets; ++i) M = __builtin_fmaxf(M, out_m[0][i * p.group + row]);
+            L = 0.f;
+#pragma unroll
+            for (int c = 0; c < VD; ++c) acc[c] = 0.f;
+            for (int i = 0; i < sets; ++i) {
+                const float f = __builtin_amdgcn_exp2f(out_m[0][i * p.group + row] - M);
+                L = __builtin_fmaf(f, out_l[0][i * p.group + row], L);
+#pragma unroll
+                for (int c = 0; c < VD; ++c) acc[c] = __builtin_fmaf(f, out_o[0][i * p.group + row][d0 + c], acc[c]);
+            }
+            single_store<DT, VD>(p, j.token, j.head * p.group + row, d0, acc, L == 0.f ? 0.f : 1.f / L);
+        }
+        __syncthreads();
     }
 }
 
