@@ -53,7 +53,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, in
 // take it times their weight.  One key after the other, the weights formed anew; this is for results that end as infinities
 // and NaN, not for speed.
 template <int DT, int DP>
-__device__ __forceinline__ void add_not_finite(const AttnArgs& p, f32x16 (&o)[DP / 32], float m, int k0, const SeqInfo& si, const int* pages,
+__device__ __forceinline__ void add_not_finite(const AttnArgs& p, f32x16 (&o)[DP / 32], float m, int k0, const SeqInfo& si, const __attribute__((address_space(4))) int* pages,
                                                          int head, int token, int qh, int lo, int hi, int h) {
     const unsigned short* const q = reinterpret_cast<const unsigned short*>(p.Q) + token * p.ldq + (long long)qh * p.dim;
     for (int key = k0; key < min(k0 + ATTN_BLOCK_KEYS, si.kv); ++key) {
@@ -119,75 +119,111 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
         q[s] = row_on && d < p.dim ? ld16(p.Q + (token * p.ldq + (long long)qh * p.dim + d) * 2) : i32x4{0, 0, 0, 0};
     }
 
-    // ---- copies: 16 bytes a thread, thread's chunk of rows tid / CPR + PASS i of a tile
+    // ---- copies: 16 bytes a thread, thread's chunk of rows tid / CPR + PASS i of a tile.  A wavefront's rows of a pass lie in one block
+    // of sixteen keys: its place is the wavefront's, through the scalar cache, a tile ahead of the copies; a thread's offset
+    // from it does not change.  No load has a condition: a chunk beyond the head's values is its row's first, a block without
+    // keys the last one with some.
     constexpr int CPR = I8 ? T::PITCH / 32 : T::PITCH / 16, PASS = 256 / CPR, NP = KEYS / PASS;
-    const int chunk = tid % CPR, crow = tid / CPR;
-    const bool chunk_on = chunk * 16 < p.dim * (I8 ? 1 : 2);
-    const int* const pages = p.table + seq * p.ld_table;
+    static_assert(64 / CPR <= 16, "a wavefront's rows in one block");
+    const int chunk = tid % CPR, crow = tid / CPR, wrow = wave * (64 / CPR);
     const int row_bytes = p.dim * (I8 ? 1 : 2);
-    i32x4 kreg[NP], vreg[NP];
-    float scale_reg = 0.f;
-    auto load_tile = [&](int kt) {
+    const unsigned my_off = (unsigned)((crow & 15) * row_bytes + (chunk * 16 < row_bytes ? chunk * 16 : 0));
+    typedef const __attribute__((address_space(4))) int ScalarInt;
+    ScalarInt* const pages = (ScalarInt*)(p.table + seq * p.ld_table);
+    auto block_of = [&](int kt, int i) { return (unsigned)min(kt * KEYS + wrow + i * PASS, si.kv - 1) >> 4; };
+    int entries[NP];
+    auto load_entries = [&](int kt) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) entries[i] = pages[page_of(p, block_of(kt, i))];
+    };
+    // 16-bit caches: straight into LDS, each lane's chunk from where its place wants it (a chunk of a key beyond the head's values:
+    // zeros, since what is not finite would not vanish against the zeros of the queries).
+    const int k_chunk = chunk ^ T::k_swizzle(crow), v_chunk = chunk ^ T::v_swizzle(crow);   // (a pass is a multiple of the swizzles' period)
+    const unsigned k_off = (unsigned)((crow & 15) * row_bytes + k_chunk * 16), v_off = (unsigned)((crow & 15) * row_bytes + (v_chunk * 16 < row_bytes ? v_chunk * 16 : 0));
+    const bool k_zero = k_chunk * 16 >= row_bytes;
+    // int8: through registers, where they are widened
+    i32x4 kreg[I8 ? NP : 1], vreg[I8 ? NP : 1];
+    float k_scale_reg = 0.f, v_scale_reg = 0.f;
+    constexpr int PER = 64 / CPR;
+    auto load_tile = [&](int kt, int stage) {
+        long long at[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int key = kt * KEYS + crow + i * PASS;
-            kreg[i] = vreg[i] = i32x4{0, 0, 0, 0};
-            if (key < si.kv && chunk_on) {
-                const unsigned block = (unsigned)key >> 4, pi = page_of(p, block);
-                const long long at = (block_place(p, block, pi, pages[pi], head) + (key & 15)) * row_bytes + chunk * 16;
-                kreg[i] = ld16(p.K + at);
-                vreg[i] = ld16(p.V + at);
-            }
+            const unsigned block = block_of(kt, i);
+            at[i] = block_place(p, block, page_of(p, block), entries[i], head);
         }
-        if constexpr (I8) {
-            const int key = kt * KEYS + (tid & 63);
-            scale_reg = 0.f;
-            if (tid < 128 && key < si.kv) {
-                const unsigned block = (unsigned)key >> 4, pi = page_of(p, block);
-                const long long at = block_place(p, block, pi, pages[pi], head) + (key & 15);
-                scale_reg = (tid < 64 ? p.ks : p.vs)[at];
+        if constexpr (!I8) {
+            char* const to = smem + stage * T::STAGE + wave * 1024;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const char* src = p.K + at[i] * row_bytes + k_off;
+                if (p.dim < DP) src = k_zero ? g_zero_chunk : src;
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)(to + i * 4096), 16, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p.V + at[i] * row_bytes + v_off),
+                                                 (__attribute__((address_space(3))) void*)(to + T::HALF + i * 4096), 16, 0, 0);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) kreg[i] = ld16g(p.K + at[i] * row_bytes + my_off);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) vreg[i] = ld16g(p.V + at[i] * row_bytes + my_off);
+            // (a wavefront's lanes in the order of its keys: PER of a pass)
+            long long key = at[0] + (wrow & 15) + lane;
+#pragma unroll
+            for (int i = 1; i < NP; ++i)
+                if (lane >= i * PER) key = at[i] + (wrow & 15) + lane - i * PER;
+            if (lane < NP * PER) {
+                k_scale_reg = p.ks[key];
+                v_scale_reg = p.vs[key];
             }
         }
     };
     int* const special = reinterpret_cast<int*>(smem + 2 * T::STAGE);   // per stage: a tile whose V holds something not finite
-    auto write_tile = [&](int kt, int stage) {
+    // what is left to do of a tile once its loads have come back (all wavefronts', then a barrier)
+    auto finish_tile = [&](int kt, int stage) {
         char* const ks = smem + stage * T::STAGE;
         char* const vs = ks + T::HALF;
-        bool bad = false;
+        if constexpr (I8) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const int r = crow + i * PASS;
-            if constexpr (I8) {
+            for (int i = 0; i < NP; ++i) {
+                const int r = crow + i * PASS;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int c = 2 * chunk + e;
                     *reinterpret_cast<i32x4*>(ks + r * T::PITCH + ((c ^ T::k_swizzle(r)) * 16)) = widen8<DT>(kreg[i][2 * e], kreg[i][2 * e + 1]);
                     *reinterpret_cast<i32x4*>(vs + r * T::PITCH + ((c ^ T::v_swizzle(r)) * 16)) = widen8<DT>(vreg[i][2 * e], vreg[i][2 * e + 1]);
                 }
-            } else {
-                *reinterpret_cast<i32x4*>(ks + r * T::PITCH + ((chunk ^ T::k_swizzle(r)) * 16)) = kreg[i];
-                // a key that some rows of the tile do not see must not reach them as 0 times infinity: such values stay out of
-                // the product and are added one by one, where they are seen
-                if (kt * KEYS < full_from || (kt + 1) * KEYS > full_to) {
-                    if (any_not_finite<DT>(vreg[i])) {
+            }
+            float* const f = reinterpret_cast<float*>(vs + T::HALF);
+            if (lane < NP * PER) {
+                const int key = wrow + lane % PER + lane / PER * PASS;
+                float l, v;
+                value_scale(v_scale_reg, l, v);
+                f[key] = k_scale_reg * p.c;
+                f[key + KEYS] = l;
+                f[key + 2 * KEYS] = v;
+            }
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            // a key that some rows of the tile do not see must not reach them as 0 times infinity: zeros behind the last key, and
+            // what is not finite stays out of the product and is added one by one, where it is seen.  (The thread's own chunks.)
+            if (kt * KEYS < full_from || (kt + 1) * KEYS > full_to) {
+                bool bad = false;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    i32x4* const at = reinterpret_cast<i32x4*>(vs + i * 4096 + tid * 16);
+                    i32x4 v = *at;
+                    if (kt * KEYS + crow + i * PASS >= si.kv) v = i32x4{0, 0, 0, 0};
+                    if (any_not_finite<DT>(v)) {
                         bad = true;
 #pragma unroll
-                        for (int d = 0; d < 4; ++d) vreg[i][d] = only_finite<DT>(vreg[i][d]);
+                        for (int d = 0; d < 4; ++d) v[d] = only_finite<DT>(v[d]);
                     }
+                    *at = v;
                 }
-                *reinterpret_cast<i32x4*>(vs + r * T::PITCH + ((chunk ^ T::v_swizzle(r)) * 16)) = vreg[i];
-            }
-        }
-        if (bad) special[stage] = kt;
-        if constexpr (I8) {
-            float* const f = reinterpret_cast<float*>(vs + T::HALF);
-            if (tid < 64) {
-                f[tid] = scale_reg * p.c;
-            } else if (tid < 128) {
-                float l, v;
-                value_scale(scale_reg, l, v);
-                f[tid] = l;
-                f[tid + 64] = v;
+                if (bad) special[stage] = kt;
             }
         }
     };
@@ -202,13 +238,18 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     if (tid < 2) special[tid] = -1;
     __syncthreads();
     if (t1 > t0) {
-        load_tile(t0);
-        write_tile(t0, 0);
+        load_entries(t0);
+        load_tile(t0, 0);
+        load_entries(t0 + 1);
+        finish_tile(t0, 0);
     }
     __syncthreads();
     for (int kt = t0; kt < t1; ++kt) {
         const int stage = (kt - t0) & 1;
-        if (kt + 1 < t1) load_tile(kt + 1);
+        if (kt + 1 < t1) {
+            load_tile(kt + 1, stage ^ 1);
+            load_entries(kt + 2);
+        }
         const int k0 = kt * KEYS;
         // (a wavefront whose rows see nothing of the tile leaves it out)
         if (wave_on && k0 < w_to && k0 + KEYS > w_from) {
@@ -315,7 +356,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
                 if (__builtin_expect(special[stage] == kt, 0)) add_not_finite<DT, DP>(p, o, m, k0, si, pages, head, token, qh, my_lo, row_on ? my_hi : 0, h);
             }
         }
-        if (kt + 1 < t1) write_tile(kt + 1, stage ^ 1);
+        if (kt + 1 < t1) finish_tile(kt + 1, stage ^ 1);
         __syncthreads();
     }
 
