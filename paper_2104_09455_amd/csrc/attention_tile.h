@@ -91,7 +91,12 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     if (!find_tile(p, (int)blockIdx.x / p.heads, T::ROWS, seq, tile, tiles)) return;
     seq = __builtin_amdgcn_readfirstlane(seq);
     tile = tiles - 1 - __builtin_amdgcn_readfirstlane(tile);   // (the rows that see most first)
-    const SeqInfo si = seq_info(p, seq);
+    // (what is the workgroup's or the wavefront's goes into scalar registers, or branches and addresses end up in vector code)
+    auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    SeqInfo si = seq_info(p, seq);
+    si.q0 = scalar(si.q0);
+    si.nq = scalar(si.nq);
+    si.kv = scalar(si.kv);
     const int split = blockIdx.y, rows = si.nq * p.group, before = si.kv - si.nq;
     const int chunks = max(1, (si.kv + p.tile_chunk - 1) / p.tile_chunk);
     if (split >= chunks) return;
@@ -106,9 +111,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     const bool row_on = row0 + wave * 32 + col < rows;
     const int my_lo = lo_of(my_row), my_hi = hi_of(my_row);
     const int from = max(lo_of(row0), split * p.tile_chunk), to = min(hi_of(row_end), min(si.kv, (split + 1) * p.tile_chunk));
-    const int full_from = lo_of(row_end), full_to = hi_of(row0);            // keys that all rows of the workgroup see
-    const int w_from = lo_of(wrow0), w_to = hi_of(wrow_end), w_full_from = lo_of(wrow_end), w_full_to = hi_of(wrow0);
-    const int t0 = from / KEYS, t1 = to > from ? (to + KEYS - 1) / KEYS : t0;   // tiles of keys
+    const int full_from = scalar(lo_of(row_end)), full_to = scalar(hi_of(row0));            // keys that all rows of the workgroup see
+    const int w_from = scalar(lo_of(wrow0)), w_to = scalar(hi_of(wrow_end)), w_full_from = scalar(lo_of(wrow_end)), w_full_to = scalar(hi_of(wrow0));
+    const int t0 = scalar(from / KEYS), t1 = scalar(to > from ? (to + KEYS - 1) / KEYS : t0);   // tiles of keys
 
     // ---- this lane's query, as the fragments of the first product want it: values 16 s + 8 h .. + 7 of its row
     const int token = si.q0 + my_row / p.group, qh = head * p.group + my_row % p.group;
@@ -283,13 +288,14 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
             }
             const bool masked = k0 < w_full_from || k0 + KEYS > w_full_to;
             if (masked) {
+                asm volatile("");   // (a branch: selects in its place would cost every tile 128 instructions)
+                const int first = k0 + 4 * h - my_lo;
+                const unsigned seen = (unsigned)max(my_hi - my_lo, 0);
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int key = k0 + 32 * kb + 8 * (r >> 2) + 4 * h + (r & 3);
-                        s[kb][r] = key >= my_lo && key < my_hi ? s[kb][r] : -__builtin_huge_valf();
-                    }
+                    for (int r = 0; r < 16; ++r)
+                        s[kb][r] = (unsigned)(first + 32 * kb + 8 * (r >> 2) + (r & 3)) < seen ? s[kb][r] : -__builtin_huge_valf();
             }
             // ---- the running maximum
             float top = s[0][0];
