@@ -10,9 +10,9 @@ struct AttnTile {
     static constexpr int PITCH = DP <= 64 ? 128 : 256;            // bytes of a key's row in LDS
     static constexpr int ROWS = 128;                              // rows of a workgroup
     static constexpr int KEYS = ATTN_BLOCK_KEYS;
-    static constexpr int HALF = KEYS * PITCH;                     // K, or V
-    static constexpr int STAGE = 2 * HALF + 3 * KEYS * 4;         // and three floats a key
-    static constexpr int LDS_BYTES = 2 * STAGE + 16;
+    static constexpr int K_STAGE = KEYS * PITCH + 2 * KEYS * 4;   // K, and two floats a key (int8)
+    static constexpr int V_STAGE = KEYS * PITCH + KEYS * 4;       // V, and one
+    static constexpr int LDS_BYTES = 2 * (K_STAGE + V_STAGE) + 16;
     // 16-byte chunk c of row r lies at chunk c ^ swizzle(r): the 16 rows that a fragment of K is read from at once, and the
     // 4 (x 64 bytes) of V, lie in different banks
     static __device__ __forceinline__ int k_swizzle(int r) { return PITCH == 256 ? r & 15 : (r >> 1) & 7; }
@@ -106,13 +106,13 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     auto hi_of = [&](int r) { return p.causal ? min(before + r / p.group + 1, si.kv) : si.kv; };
     const int row0 = tile * T::ROWS, row_end = min(row0 + T::ROWS, rows) - 1;
     const int wrow0 = min(row0 + wave * 32, rows - 1), wrow_end = min(row0 + wave * 32 + 31, rows - 1);
-    const bool wave_on = row0 + wave * 32 < rows;
+    const bool wave_on = scalar(row0 + wave * 32 < rows);
     const int my_row = min(row0 + wave * 32 + col, rows - 1);
     const bool row_on = row0 + wave * 32 + col < rows;
     const int my_lo = lo_of(my_row), my_hi = hi_of(my_row);
     const int from = max(lo_of(row0), split * p.tile_chunk), to = min(hi_of(row_end), min(si.kv, (split + 1) * p.tile_chunk));
     const int full_from = scalar(lo_of(row_end)), full_to = scalar(hi_of(row0));            // keys that all rows of the workgroup see
-    const int w_from = scalar(lo_of(wrow0)), w_to = scalar(hi_of(wrow_end)), w_full_from = scalar(lo_of(wrow_end)), w_full_to = scalar(hi_of(wrow0));
+    const int w_full_from = scalar(lo_of(wrow_end)), w_full_to = scalar(hi_of(wrow0));
     const int t0 = scalar(from / KEYS), t1 = scalar(to > from ? (to + KEYS - 1) / KEYS : t0);   // tiles of keys
 
     // ---- this lane's query, as the fragments of the first product want it: values 16 s + 8 h .. + 7 of its row
@@ -128,9 +128,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     // of sixteen keys: its place is the wavefront's, through the scalar cache, a tile ahead of the copies; a thread's offset
     // from it does not change.  No load has a condition: a chunk beyond the head's values is its row's first, a block without
     // keys the last one with some.
-    constexpr int CPR = I8 ? T::PITCH / 32 : T::PITCH / 16, PASS = 256 / CPR, NP = KEYS / PASS;
-    static_assert(64 / CPR <= 16, "a wavefront's rows in one block");
-    const int chunk = tid % CPR, crow = tid / CPR, wrow = wave * (64 / CPR);
+    constexpr int CPR = I8 ? T::PITCH / 32 : T::PITCH / 16, PASS = 256 / CPR, NP = KEYS / PASS, PER = 64 / CPR;
+    static_assert(PER <= 16, "a wavefront's rows in one block");
+    const int chunk = tid % CPR, crow = tid / CPR, wrow = wave * PER;
     const int row_bytes = p.dim * (I8 ? 1 : 2);
     const unsigned my_off = (unsigned)((crow & 15) * row_bytes + (chunk * 16 < row_bytes ? chunk * 16 : 0));
     typedef const __attribute__((address_space(4))) int ScalarInt;
@@ -141,6 +141,14 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) entries[i] = pages[page_of(p, block_of(kt, i))];
     };
+    long long at[NP];   // the places of the tile whose entries were loaded last but one: its keys' now, its values' a tile later
+    auto place = [&](int kt) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const unsigned block = block_of(kt, i);
+            at[i] = block_place(p, block, page_of(p, block), entries[i], head);
+        }
+    };
     // 16-bit caches: straight into LDS, each lane's chunk from where its place wants it (a chunk of a key beyond the head's values:
     // zeros, since what is not finite would not vanish against the zeros of the queries).
     const int k_chunk = chunk ^ T::k_swizzle(crow), v_chunk = chunk ^ T::v_swizzle(crow);   // (a pass is a multiple of the swizzles' period)
@@ -148,87 +156,107 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     const bool k_zero = k_chunk * 16 >= row_bytes;
     // int8: through registers, where they are widened
     i32x4 kreg[I8 ? NP : 1], vreg[I8 ? NP : 1];
-    float k_scale_reg = 0.f, v_scale_reg = 0.f;
-    constexpr int PER = 64 / CPR;
-    auto load_tile = [&](int kt, int stage) {
-        long long at[NP];
+    float kc_reg = 0.f, kt_reg = 0.f, vt_reg = 0.f;
+    char* const k_lds = smem;
+    char* const v_lds = smem + 2 * T::K_STAGE;
+    auto to_lds = [&](const char* src, char* dst) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+    };
+    // a lane's key of the wavefront's, in the order of its passes, among a head's tokens
+    auto scale_place = [&]() {
+        long long key = at[0] + (wrow & 15) + lane;
+#pragma unroll
+        for (int i = 1; i < NP; ++i)
+            if (lane >= i * PER) key = at[i] + (wrow & 15) + lane - i * PER;
+        return key;
+    };
+    auto load_k = [&](int stage) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const unsigned block = block_of(kt, i);
-            at[i] = block_place(p, block, page_of(p, block), entries[i], head);
-        }
-        if constexpr (!I8) {
-            char* const to = smem + stage * T::STAGE + wave * 1024;
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const char* src = p.K + at[i] * row_bytes + k_off;
+            const char* src = p.K + at[i] * row_bytes;
+            if constexpr (I8) {
+                kreg[i] = ld16g(src + my_off);
+            } else {
+                src += k_off;
                 if (p.dim < DP) src = k_zero ? g_zero_chunk : src;
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)(to + i * 4096), 16, 0, 0);
+                to_lds(src, k_lds + stage * T::K_STAGE + wave * 1024 + i * 4096);
             }
+        }
+        if constexpr (I8)
+            if (lane < NP * PER) {
+                const long long key = scale_place();
+                kc_reg = p.ks[key];
+                kt_reg = p.vs[key];
+            }
+    };
+    auto load_v = [&](int stage) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const char* const src = p.V + at[i] * row_bytes;
+            if constexpr (I8) vreg[i] = ld16g(src + my_off);
+            else to_lds(src + v_off, v_lds + stage * T::V_STAGE + wave * 1024 + i * 4096);
+        }
+        if constexpr (I8)
+            if (lane < NP * PER) vt_reg = p.vs[scale_place()];
+    };
+    // what is left to do of a tile's keys or values once their loads have come back (all wavefronts', then a barrier)
+    const int scale_key = wrow + lane % PER + lane / PER * PASS;
+    auto finish_k = [&](int stage) {
+        if constexpr (I8) {
+            char* const ks = k_lds + stage * T::K_STAGE;
 #pragma unroll
             for (int i = 0; i < NP; ++i)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p.V + at[i] * row_bytes + v_off),
-                                                 (__attribute__((address_space(3))) void*)(to + T::HALF + i * 4096), 16, 0, 0);
-        } else {
 #pragma unroll
-            for (int i = 0; i < NP; ++i) kreg[i] = ld16g(p.K + at[i] * row_bytes + my_off);
-#pragma unroll
-            for (int i = 0; i < NP; ++i) vreg[i] = ld16g(p.V + at[i] * row_bytes + my_off);
-            // (a wavefront's lanes in the order of its keys: PER of a pass)
-            long long key = at[0] + (wrow & 15) + lane;
-#pragma unroll
-            for (int i = 1; i < NP; ++i)
-                if (lane >= i * PER) key = at[i] + (wrow & 15) + lane - i * PER;
+                for (int e = 0; e < 2; ++e) {
+                    const int r = crow + i * PASS, c = 2 * chunk + e;
+                    *reinterpret_cast<i32x4*>(ks + r * T::PITCH + ((c ^ T::k_swizzle(r)) * 16)) = widen8<DT>(kreg[i][2 * e], kreg[i][2 * e + 1]);
+                }
+            float* const f = reinterpret_cast<float*>(ks + KEYS * T::PITCH);
             if (lane < NP * PER) {
-                k_scale_reg = p.ks[key];
-                v_scale_reg = p.vs[key];
+                float log2_t, inv_t;
+                value_scale(kt_reg, log2_t, inv_t);
+                f[scale_key] = kc_reg * p.c;
+                f[scale_key + KEYS] = log2_t;
             }
         }
     };
-    int* const special = reinterpret_cast<int*>(smem + 2 * T::STAGE);   // per stage: a tile whose V holds something not finite
-    // what is left to do of a tile once its loads have come back (all wavefronts', then a barrier)
-    auto finish_tile = [&](int kt, int stage) {
-        char* const ks = smem + stage * T::STAGE;
-        char* const vs = ks + T::HALF;
+    int* const special = reinterpret_cast<int*>(smem + 2 * (T::K_STAGE + T::V_STAGE));   // whether values that are not finite were left out
+    auto partial = [&](int kt) { return kt * KEYS < full_from || (kt + 1) * KEYS > full_to; };   // (some rows do not see all of the tile)
+    auto finish_v = [&](int kt, int stage) {
+        char* const vs = v_lds + stage * T::V_STAGE;
         if constexpr (I8) {
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                const int r = crow + i * PASS;
+            for (int i = 0; i < NP; ++i)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const int c = 2 * chunk + e;
-                    *reinterpret_cast<i32x4*>(ks + r * T::PITCH + ((c ^ T::k_swizzle(r)) * 16)) = widen8<DT>(kreg[i][2 * e], kreg[i][2 * e + 1]);
+                    const int r = crow + i * PASS, c = 2 * chunk + e;
                     *reinterpret_cast<i32x4*>(vs + r * T::PITCH + ((c ^ T::v_swizzle(r)) * 16)) = widen8<DT>(vreg[i][2 * e], vreg[i][2 * e + 1]);
                 }
-            }
-            float* const f = reinterpret_cast<float*>(vs + T::HALF);
             if (lane < NP * PER) {
-                const int key = wrow + lane % PER + lane / PER * PASS;
-                float l, v;
-                value_scale(v_scale_reg, l, v);
-                f[key] = k_scale_reg * p.c;
-                f[key + KEYS] = l;
-                f[key + 2 * KEYS] = v;
+                float log2_t, inv_t;
+                value_scale(vt_reg, log2_t, inv_t);
+                // (a scale that is NaN makes its key's weight NaN where it is seen, and must not reach other rows as 0 times NaN)
+                reinterpret_cast<float*>(vs + KEYS * T::PITCH)[scale_key] = inv_t == inv_t ? inv_t : 0.f;
             }
         } else {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             // a key that some rows of the tile do not see must not reach them as 0 times infinity: zeros behind the last key, and
-            // what is not finite stays out of the product and is added one by one, where it is seen.  (The thread's own chunks.)
-            if (kt * KEYS < full_from || (kt + 1) * KEYS > full_to) {
+            // what is not finite stays out of the product and is added at the end, where it is seen.  (The thread's own chunks.)
+            if (partial(kt)) {
                 bool bad = false;
 #pragma unroll
                 for (int i = 0; i < NP; ++i) {
-                    i32x4* const at = reinterpret_cast<i32x4*>(vs + i * 4096 + tid * 16);
-                    i32x4 v = *at;
+                    i32x4* const here = reinterpret_cast<i32x4*>(vs + i * 4096 + tid * 16);
+                    i32x4 v = *here;
                     if (kt * KEYS + crow + i * PASS >= si.kv) v = i32x4{0, 0, 0, 0};
                     if (any_not_finite<DT>(v)) {
                         bad = true;
 #pragma unroll
                         for (int d = 0; d < 4; ++d) v[d] = only_finite<DT>(v[d]);
                     }
-                    *at = v;
+                    *here = v;
                 }
-                if (bad) special[stage] = kt;
+                if (bad) *special = 1;
             }
         }
     };
@@ -240,130 +268,210 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
         for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
     float m = ATTN_NONE, l = 0.f;   // (m: as a power of two)
 
-    if (tid < 2) special[tid] = -1;
-    __syncthreads();
-    if (t1 > t0) {
-        load_entries(t0);
-        load_tile(t0, 0);
-        load_entries(t0 + 1);
-        finish_tile(t0, 0);
-    }
-    __syncthreads();
-    for (int kt = t0; kt < t1; ++kt) {
-        const int stage = (kt - t0) & 1;
-        if (kt + 1 < t1) {
-            load_tile(kt + 1, stage ^ 1);
-            load_entries(kt + 2);
+    // ---- the pieces of a tile's way.  S^T, two blocks of 32 keys; key of register r in block kb: k0 + 32 kb + 8 (r / 4) + 4 h + r % 4
+    typedef typename MMA::Acc Scores[2];
+    auto scores = [&](int stage, Scores& s) {
+        const char* const ks = k_lds + stage * T::K_STAGE;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                const int r = kb * 32 + col;
+                const i32x4 a = *reinterpret_cast<const i32x4*>(ks + r * T::PITCH + (((2 * st + h) ^ T::k_swizzle(r)) * 16));
+                s[kb] = MMA::run(a, q[st], s[kb]);
+            }
         }
-        const int k0 = kt * KEYS;
-        // (a wavefront whose rows see nothing of the tile leaves it out)
-        if (wave_on && k0 < w_to && k0 + KEYS > w_from) {
-            const char* const ks = smem + stage * T::STAGE;
-            const char* const vs = ks + T::HALF;
-            // ---- S^T: two blocks of 32 keys
-            typename MMA::Acc s[2];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
-#pragma unroll
-                for (int st = 0; st < STEPS; ++st) {
-                    const int r = kb * 32 + col;
-                    const i32x4 a = *reinterpret_cast<const i32x4*>(ks + r * T::PITCH + (((2 * st + h) ^ T::k_swizzle(r)) * 16));
-                    s[kb] = MMA::run(a, q[st], s[kb]);
-                }
-            }
-            // key of register r in block kb: k0 + 32 kb + 8 (r / 4) + 4 h + r % 4
-            const float* const fs = reinterpret_cast<const float*>(vs + T::HALF) + 4 * h;
-            if constexpr (I8) {
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int r4 = 0; r4 < 4; ++r4) {
-                        const f32x4 kc = *reinterpret_cast<const f32x4*>(fs + 32 * kb + 8 * r4);
-                        const f32x4 lt = *reinterpret_cast<const f32x4*>(fs + KEYS + 32 * kb + 8 * r4);
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) s[kb][4 * r4 + r] = __builtin_fmaf(s[kb][4 * r4 + r], kc[r], lt[r]);
-                    }
-            }
-            const bool masked = k0 < w_full_from || k0 + KEYS > w_full_to;
-            if (masked) {
-                asm volatile("");   // (a branch: selects in its place would cost every tile 128 instructions)
-                const int first = k0 + 4 * h - my_lo;
-                const unsigned seen = (unsigned)max(my_hi - my_lo, 0);
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[kb][r] = (unsigned)(first + 32 * kb + 8 * (r >> 2) + (r & 3)) < seen ? s[kb][r] : -__builtin_huge_valf();
-            }
-            // ---- the running maximum
-            float top = s[0][0];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kb][r]);
-            if constexpr (!I8) top *= p.c;
-            if (__any(top - m > ATTN_SLACK)) {
-                top = __builtin_fmaxf(__builtin_fmaxf(top, swap_halves(top)), m);
-                const float f = __builtin_amdgcn_exp2f(m - top);
-                m = top;
-                l *= f;
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) o[b][r] *= f;
-            }
-            // ---- weights and their sum
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[kb][r] = __builtin_amdgcn_exp2f(I8 ? s[kb][r] - m : __builtin_fmaf(s[kb][r], p.c, -m));
+    };
+    auto scale_scores = [&](int stage, Scores& s) {
+        if constexpr (I8) {
+            const float* const fs = reinterpret_cast<const float*>(k_lds + stage * T::K_STAGE + KEYS * T::PITCH) + 4 * h;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
                 for (int r4 = 0; r4 < 4; ++r4) {
-                    if constexpr (I8) {
-                        f32x4 inv = *reinterpret_cast<const f32x4*>(fs + 2 * KEYS + 32 * kb + 8 * r4);
+                    const f32x4 kc = *reinterpret_cast<const f32x4*>(fs + 32 * kb + 8 * r4);
+                    const f32x4 lt = *reinterpret_cast<const f32x4*>(fs + KEYS + 32 * kb + 8 * r4);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            // (a key that is not seen may have any scale)
-                            if (masked) inv[r] = s[kb][4 * r4 + r] == 0.f ? 0.f : inv[r];
-                            l = __builtin_fmaf(s[kb][4 * r4 + r], inv[r], l);
-                        }
-                    } else {
-                        l += (s[kb][4 * r4] + s[kb][4 * r4 + 1]) + (s[kb][4 * r4 + 2] + s[kb][4 * r4 + 3]);
-                    }
+                    for (int r = 0; r < 4; ++r) s[kb][4 * r4 + r] = __builtin_fmaf(s[kb][4 * r4 + r], kc[r], lt[r]);
                 }
-            // ---- O^T += V^T P^T: sixteen keys at a time, 32 kb + 16 half + {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}
+        }
+    };
+    auto mask_scores = [&](int kt, Scores& s) {
+        const int k0 = kt * KEYS;
+        if (k0 < w_full_from || k0 + KEYS > w_full_to) {
+            asm volatile("");   // (a branch: selects in its place would cost every tile 128 instructions)
+            const int first = k0 + 4 * h - my_lo;
+            const unsigned seen = (unsigned)max(my_hi - my_lo, 0);
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    i32x4 w;
+                for (int r = 0; r < 16; ++r)
+                    s[kb][r] = (unsigned)(first + 32 * kb + 8 * (r >> 2) + (r & 3)) < seen ? s[kb][r] : -__builtin_huge_valf();
+        }
+    };
+    auto top_of = [&](const Scores& s) {
+        float top = s[0][0];
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) w[d] = pack_out16<DT>(s[kb][8 * half + 2 * d], s[kb][8 * half + 2 * d + 1]);
+        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int b = 0; b < BLOCKS; ++b) {
-                        // (a transposing read: sixteen lanes bring four keys' rows of sixteen values and get a column each)
-                        i32x4 a;
+            for (int r = 0; r < 16; ++r) top = __builtin_fmaxf(top, s[kb][r]);
+        return I8 ? top : top * p.c;
+    };
+    auto move_maximum = [&](float top) {
+        if (__any(top - m > ATTN_SLACK)) {
+            top = __builtin_fmaxf(__builtin_fmaxf(top, swap_halves(top)), m);
+            const float f = __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            l *= f;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const int r = 32 * kb + 16 * half + 8 * e + 4 * h + ((lane & 15) >> 2);
-                            const int byte = 64 * b + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-                            const i32x2 v = read_transposed(vs + r * T::PITCH + (((byte >> 4) ^ T::v_swizzle(r)) * 16) + (byte & 15));
-                            a[2 * e] = v[0];
-                            a[2 * e + 1] = v[1];
-                        }
-                        o[b] = MMA::run(a, w, o[b]);
-                    }
+            for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[b][r] *= f;
+        }
+    };
+    // a fragment of V^T of the second product: sixteen keys, 32 kb + 16 half + {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}, block b of its values.
+    // (Transposing reads: sixteen lanes bring four keys' rows of sixteen values and get a column each.)
+    auto v_fragment = [&](int stage, int kb, int half, int b) {
+        i32x4 a;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 32 * kb + 16 * half + 8 * e + 4 * h + ((lane & 15) >> 2);
+            const int byte = 64 * b + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+            const i32x2 v = read_transposed(v_lds + stage * T::V_STAGE + r * T::PITCH + (((byte >> 4) ^ T::v_swizzle(r)) * 16) + (byte & 15));
+            a[2 * e] = v[0];
+            a[2 * e + 1] = v[1];
+        }
+        return a;
+    };
+
+    // One tile: its scores (now) have been formed, masked and seen by the maximum; those of the next are formed beside its weights,
+    // so that a wavefront has work for the matrix unit and for the vector unit at the same time.  The order of the instructions is
+    // the one written here (sched_barrier): AHEAD fragments are on their way from LDS before the first is used, and behind each
+    // matrix instruction (32 cycles) come the next read and about as many cycles of weights.  Left to itself the compiler reads
+    // each fragment into the same registers and waits for it.
+    auto step = [&](int kt, int stage, Scores& now, Scores& next) {
+        constexpr int NS = 2 * STEPS, NV = 4 * BLOCKS, AHEAD = 6 < NS ? 6 : NS, V_AHEAD = 4;
+        constexpr int FIRST = 20;   // weights formed beside the scores: at least the first block's, 16 of 32
+        const float* const inv_of = reinterpret_cast<const float*>(v_lds + stage * T::V_STAGE + KEYS * T::PITCH) + 4 * h;
+        int w[4][4];
+        f32x4 inv;
+        float sum = 0.f;
+        auto weight = [&](int e) {
+            const int kb = e >> 4, r = e & 15;
+            if constexpr (I8) {
+                if ((e & 3) == 0) inv = *reinterpret_cast<const f32x4*>(inv_of + 32 * kb + 8 * (r >> 2));
+                now[kb][r] = __builtin_amdgcn_exp2f(now[kb][r] - m);
+                sum = __builtin_fmaf(now[kb][r], inv[e & 3], sum);
+            } else {
+                now[kb][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(now[kb][r], p.c, -m));
+                sum += now[kb][r];
+            }
+            if (e & 1) w[e >> 3][(e & 7) >> 1] = pack_out16<DT>(now[kb][r - 1], now[kb][r]);
+        };
+        {
+            i32x4 a[AHEAD];
+            auto read = [&](int i) {
+                const int r = (i / STEPS) * 32 + col;
+                a[i % AHEAD] = *reinterpret_cast<const i32x4*>(k_lds + (stage ^ 1) * T::K_STAGE + r * T::PITCH + (((2 * (i % STEPS) + h) ^ T::k_swizzle(r)) * 16));
+            };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) read(i);
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) next[kb][r] = 0.f;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < NS; ++i) {
+                next[i / STEPS] = MMA::run(a[i % AHEAD], q[i % STEPS], next[i / STEPS]);
+                if (i + AHEAD < NS) read(i + AHEAD);
+#pragma unroll
+                for (int e = i * FIRST / NS; e < (i + 1) * FIRST / NS; ++e) {
+                    weight(e);
+                    if (e & 1) asm volatile("" : "+v"(w[e >> 3][(e & 7) >> 1]), "+v"(sum));   // (here, not where they are used)
                 }
-            if constexpr (!I8) {
-                if (__builtin_expect(special[stage] == kt, 0)) add_not_finite<DT, DP>(p, o, m, k0, si, pages, head, token, qh, my_lo, row_on ? my_hi : 0, h);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (kt + 1 < t1) finish_tile(kt + 1, stage ^ 1);
+        i32x4 a[V_AHEAD];
+        auto read = [&](int i) { a[i % V_AHEAD] = v_fragment(stage, i / (2 * BLOCKS), i / BLOCKS % 2, i % BLOCKS); };
+#pragma unroll
+        for (int i = 0; i < V_AHEAD; ++i) read(i);
+        if constexpr (!I8) mask_scores(kt + 1, next);
+        __builtin_amdgcn_sched_barrier(0);
+        float top = next[0][0];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            o[i % BLOCKS] = MMA::run(a[i % V_AHEAD], i32x4{w[i / BLOCKS][0], w[i / BLOCKS][1], w[i / BLOCKS][2], w[i / BLOCKS][3]}, o[i % BLOCKS]);
+            if (i + V_AHEAD < NV) read(i + V_AHEAD);
+            if (i < NV / 2) {
+#pragma unroll
+                for (int e = FIRST + i * (32 - FIRST) / (NV / 2); e < FIRST + (i + 1) * (32 - FIRST) / (NV / 2); ++e) weight(e);
+            } else if constexpr (!I8) {
+                const int j = i - NV / 2;
+#pragma unroll
+                for (int e = j * 32 / (NV / 2); e < (j + 1) * 32 / (NV / 2); ++e) top = __builtin_fmaxf(top, next[e >> 4][e & 15]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        l += sum;
+        if constexpr (I8) {
+            scale_scores(stage ^ 1, next);
+            mask_scores(kt + 1, next);
+            top = top_of(next);
+        } else {
+            top *= p.c;
+        }
+        move_maximum(top);
+    };
+
+    if (tid == 0) *special = 0;
+    __syncthreads();
+    Scores s0, s1;
+    if (t1 > t0) {
+        load_entries(t0);
+        place(t0);
+        load_entries(t0 + 1);
+        load_k(0);
+        load_v(0);
+        finish_k(0);
+        finish_v(t0, 0);
+        place(t0 + 1);
+        load_entries(t0 + 2);
+        load_k(1);
+        finish_k(1);
+        if constexpr (!I8) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
+        scores(0, s0);
+        scale_scores(0, s0);
+        mask_scores(t0, s0);
+        move_maximum(top_of(s0));
+        __syncthreads();   // (the first keys' place is the third's)
+    }
+    // tile kt + 2's keys and kt + 1's values come in while kt + 1's keys and kt's values are used (beyond the last tile: whatever
+    // block_of gives, unused)
+    auto turn = [&](int kt, auto stage_c, Scores& now, Scores& next) {
+        constexpr int stage = decltype(stage_c)::value;
+        load_v(stage ^ 1);
+        place(kt + 2);
+        load_entries(kt + 3);
+        load_k(stage);
+        if (wave_on) step(kt, stage, now, next);
+        finish_k(stage);
+        finish_v(kt + 1, stage ^ 1);
+        __syncthreads();
+    };
+    for (int kt = t0; kt < t1; kt += 2) {
+        turn(kt, std::integral_constant<int, 0>(), s0, s1);
+        if (kt + 1 < t1) turn(kt + 1, std::integral_constant<int, 1>(), s1, s0);
+    }
+    if constexpr (!I8) {
+        if (__builtin_expect(*special != 0, 0)) {
+            for (int kt = t0; kt < t1; ++kt)
+                if (partial(kt)) add_not_finite<DT, DP>(p, o, m, kt * KEYS, si, pages, head, token, qh, my_lo, row_on ? my_hi : 0, h);
+        }
     }
 
     // ---- out: this lane's row, values 32 b + 8 (r / 4) + 4 h + r % 4
