@@ -479,7 +479,8 @@ size_t abft_linear_scaled_workspace_bytes(int M, int N, int K, int mode);
  *                     (all 16-byte aligned, else ABFT_E_LD)
  *   dtype           : ABFT_I8 (integers with a scale for each token and head, the rule of abft_quantize_rows over
  *                     head_dim values), or ABFT_F16 / ABFT_BF16 (the values as they are)
- *   page_size       : a multiple of 16 up to 4096 (ABFT_E_VALUE); pages * page_size below 2^31
+ *   page_size       : a multiple of 16 up to 4096 (ABFT_E_VALUE); pages * page_size and pages *
+ *                     heads below 2^31 (ABFT_E_SHAPE)
  *   head_dim        : a multiple of 16 up to 128 (ABFT_E_SHAPE)
  * The struct is read during a call only; the buffers are the caller's. */
 typedef struct {

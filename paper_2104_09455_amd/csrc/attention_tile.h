@@ -53,7 +53,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, in
 // take it times their weight.  One key after the other, the weights formed anew; this is for results that end as infinities
 // and NaN, not for speed.
 template <int DT, int DP>
-__device__ __forceinline__ void add_not_finite(const AttnArgs& p, f32x16 (&o)[DP / 32], float m, int k0, const SeqInfo& si, const __attribute__((address_space(4))) int* pages,
+__device__ __forceinline__ void add_not_finite(const AttnArgs& p, f32x16 (&o)[DP / 32], float m, int k0, const SeqInfo& si, const int* pages,
                                                          int head, int token, int qh, int lo, int hi, int h) {
     const unsigned short* const q = reinterpret_cast<const unsigned short*>(p.Q) + token * p.ldq + (long long)qh * p.dim;
     for (int key = k0; key < min(k0 + ATTN_BLOCK_KEYS, si.kv); ++key) {
@@ -76,7 +76,8 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& p, f32x16 (&o)[DP
     }
 }
 
-template <int DT, bool I8, int DP>
+// PAD: heads of fewer than DP values (16-bit caches; int8 ones do not care)
+template <int DT, bool I8, int DP, bool PAD>
 __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     typedef AttnTile<DP> T;
     typedef Mma<DT, 32> MMA;
@@ -125,7 +126,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     }
 
     // ---- copies: 16 bytes a thread, thread's chunk of rows tid / CPR + PASS i of a tile.  A wavefront's rows of a pass lie in one block
-    // of sixteen keys: its place is the wavefront's, through the scalar cache, a tile ahead of the copies; a thread's offset
+    // of sixteen keys: its place is the wavefront's, its page's number loaded a tile ahead of the copies; a thread's offset
     // from it does not change.  No load has a condition: a chunk beyond the head's values is its row's first, a block without
     // keys the last one with some.
     constexpr int CPR = I8 ? T::PITCH / 32 : T::PITCH / 16, PASS = 256 / CPR, NP = KEYS / PASS, PER = 64 / CPR;
@@ -133,20 +134,25 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     const int chunk = tid % CPR, crow = tid / CPR, wrow = wave * PER;
     const int row_bytes = p.dim * (I8 ? 1 : 2);
     const unsigned my_off = (unsigned)((crow & 15) * row_bytes + (chunk * 16 < row_bytes ? chunk * 16 : 0));
-    typedef const __attribute__((address_space(4))) int ScalarInt;
-    ScalarInt* const pages = (ScalarInt*)(p.table + seq * p.ld_table);
-    auto block_of = [&](int kt, int i) { return (unsigned)min(kt * KEYS + wrow + i * PASS, si.kv - 1) >> 4; };
-    int entries[NP];
-    auto load_entries = [&](int kt) {
-#pragma unroll
-        for (int i = 0; i < NP; ++i) entries[i] = pages[page_of(p, block_of(kt, i))];
-    };
-    long long at[NP];   // the places of the tile whose entries were loaded last but one: its keys' now, its values' a tile later
+    const int* const pages = p.table + seq * p.ld_table;
+    // lane i: pass i's block of a tile
+    auto block_of = [&](int kt) { return (unsigned)min(kt * KEYS + wrow + min(lane, NP - 1) * PASS, si.kv - 1) >> 4; };
+    int entry = 0;
+    auto load_entries = [&](int kt) { entry = pages[page_of(p, block_of(kt))]; };
+    // the places of the tile whose entries were loaded last but one, in bytes from the cache's start: its keys' now, its values' a
+    // tile later.  Formed in lanes, a pass each, and handed to scalar registers.
+    long long at[NP], key_at[I8 ? NP : 1];   // (int8: among a head's tokens, too, for the scales)
+    const unsigned head_bytes = (unsigned)(p.page_size * row_bytes);
     auto place = [&](int kt) {
+        const unsigned block = block_of(kt), page = min((unsigned)max(entry, 0), (unsigned)(p.pages - 1)), in_page = block - page_of(p, block) * p.page_blocks;
+        const unsigned long long of_head = page * (unsigned)p.heads + (unsigned)head;
+        const unsigned long long lane_at = of_head * head_bytes + in_page * (unsigned)(16 * row_bytes);
 #pragma unroll
-        for (int i = 0; i < NP; ++i) {
-            const unsigned block = block_of(kt, i);
-            at[i] = block_place(p, block, page_of(p, block), entries[i], head);
+        for (int i = 0; i < NP; ++i) at[i] = (long long)readlane(lane_at, i);
+        if constexpr (I8) {
+            const unsigned long long lane_key = of_head * (unsigned)p.page_size + in_page * 16;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) key_at[i] = (long long)readlane(lane_key, i);
         }
     };
     // 16-bit caches: straight into LDS, each lane's chunk from where its place wants it (a chunk of a key beyond the head's values:
@@ -164,21 +170,23 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     };
     // a lane's key of the wavefront's, in the order of its passes, among a head's tokens
     auto scale_place = [&]() {
-        long long key = at[0] + (wrow & 15) + lane;
+        long long key = key_at[0];
+        if constexpr (I8) {
 #pragma unroll
-        for (int i = 1; i < NP; ++i)
-            if (lane >= i * PER) key = at[i] + (wrow & 15) + lane - i * PER;
-        return key;
+            for (int i = 1; i < NP; ++i)
+                if (lane >= i * PER) key = key_at[i];
+        }
+        return key + (wrow & 15) + lane % PER;
     };
     auto load_k = [&](int stage) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const char* src = p.K + at[i] * row_bytes;
+            const char* src = p.K + at[i];
             if constexpr (I8) {
                 kreg[i] = ld16g(src + my_off);
             } else {
                 src += k_off;
-                if (p.dim < DP) src = k_zero ? g_zero_chunk : src;
+                if constexpr (PAD) src = k_zero ? g_zero_chunk : src;
                 to_lds(src, k_lds + stage * T::K_STAGE + wave * 1024 + i * 4096);
             }
         }
@@ -192,7 +200,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     auto load_v = [&](int stage) {
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const char* const src = p.V + at[i] * row_bytes;
+            const char* const src = p.V + at[i];
             if constexpr (I8) vreg[i] = ld16g(src + my_off);
             else to_lds(src + v_off, v_lds + stage * T::V_STAGE + wave * 1024 + i * 4096);
         }
