@@ -42,8 +42,8 @@ struct AttnArgs {
     int single, single_groups;
     unsigned* counters;                 // one for each of them, zero before and after a launch
     float *single_o, *single_ml;
-    // The others: tile_splits pieces of tile_chunk keys, and their sums, rows x splits of the same.
-    int tile_chunk, tile_splits;
+    // The others; tile_split: their keys may be divided, and the pieces' sums go here, row tiles of the same.
+    int tile_split;
     float *tile_o, *tile_ml;
 };
 
@@ -115,44 +115,5 @@ __device__ __forceinline__ void value_scale(float t, float& log2_t, float& inv_t
 
 constexpr float ATTN_NONE = -3.402823466e+38f;   // the running maximum before the first key
 constexpr float ATTN_SLACK = 8.f;                // how far (as powers of two) a value may pass it
-
-// Several workgroups' sums of one row put together by a wavefront: the i-th of n lies at place(i) among rows of sums and of (m, the
-// sum of weights).
-template <int DT, typename Place>
-__device__ __forceinline__ void attn_join_row(const AttnArgs& p, int n, Place place, const float* sums, const float* ml, int token, int qh) {
-    const int lane = threadIdx.x & 63;
-    float M = ATTN_NONE;
-    for (int i = lane; i < n; i += 64) M = __builtin_fmaxf(M, ml[2 * place(i)]);
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) M = __builtin_fmaxf(M, __shfl_xor(M, d));
-    float L = 0.f, x = 0.f, y = 0.f;
-    const int d = 2 * lane < p.dim ? 2 * lane : 0;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-        // a lane per place: its factor, 0 where nothing was seen (and no sums were left)
-        const int k = min(n - i0, 64);
-        const float part = lane < k ? ml[2 * place(i0 + lane) + 1] : 0.f;
-        const float f = part == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[2 * place(i0 + lane)] - M);
-        L = __builtin_fmaf(f, part, L);
-        // eight places' sums on their way at a time
-        for (int j = 0; j < k; j += 8) {
-            float2 v[8];
-            float fj[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                fj[u] = readlane(f, min(j + u, 63));
-                v[u] = *reinterpret_cast<const float2*>(sums + place(i0 + min(j + u, k - 1)) * p.dim + d);
-            }
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-                if (j + u < k && fj[u] != 0.f) {
-                    x = __builtin_fmaf(fj[u], v[u].x, x);
-                    y = __builtin_fmaf(fj[u], v[u].y, y);
-                }
-        }
-    }
-    L = wave_sum(L);
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    if (2 * lane < p.dim) *reinterpret_cast<int*>(p.O + (token * p.ldo + (long long)qh * p.dim + 2 * lane) * 2) = pack_out16<DT>(x * inv, y * inv);
-}
 
 }  // namespace abft

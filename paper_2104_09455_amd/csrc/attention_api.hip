@@ -26,7 +26,7 @@ constexpr int COMPUTE_UNITS = 256, COUNTERS = COMPUTE_UNITS * 4;
 // How a call's work is divided, from what the host knows of it.
 struct Division {
     int single, single_groups;
-    int tiles, tile_chunk, tile_splits;      // tiles: an upper bound of the row tiles, 0: none can be there
+    int tiles, tile_split;      // tiles: an upper bound of the row tiles, 0: none can be there; whether their keys may be divided
     size_t off_single_o, off_single_ml, off_tile_o, off_tile_ml, bytes;
 };
 Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max_kv, int q_heads) {
@@ -36,8 +36,6 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
     // sequences of one token have a kernel; where all have the same number of tokens, and more than one, there are none
     d.single = group <= ATTN_GROUP_MAX && (max_q == 1 || (long long)n * max_q != total_q);
     const bool tiled = !d.single || max_q > 1;
-    d.tile_splits = 1;
-    d.tile_chunk = (int)(cdiv(std::max(max_kv, 1), ATTN_BLOCK_KEYS) * ATTN_BLOCK_KEYS);
     if (d.single) {
         // all workgroups that the chip holds, if the keys give four units for each
         const long long units = cdiv(max_kv, SINGLE_UNIT) * n * c->heads;
@@ -46,13 +44,8 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
     }
     if (tiled) {
         d.tiles = n + (int)((long long)total_q * group / AttnTile<128>::ROWS);
-        // two workgroups per compute unit, if the keys give that many pieces of 512
-        const long long groups = (long long)d.tiles * c->heads;
-        const long long splits = std::min(cdiv(512, groups), cdiv(max_kv, 512));
-        if (splits > 1) {
-            d.tile_chunk = (int)(cdiv(cdiv(max_kv, splits), ATTN_BLOCK_KEYS) * ATTN_BLOCK_KEYS);
-            d.tile_splits = (int)cdiv(max_kv, d.tile_chunk);
-        }
+        // (with two tiles for each workgroup that the chip holds, the rows alone fill it)
+        d.tile_split = (long long)d.tiles * c->heads < 2 * TILE_SLOTS && max_kv > TILE_MIN_CHUNK * ATTN_BLOCK_KEYS;
     }
     size_t at = 0;
     auto take = [&](size_t floats) {
@@ -60,7 +53,7 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
         at = align_up(at + floats * 4, 256);
         return here;
     };
-    const size_t places = (size_t)2 * d.single_groups * group, rows = d.tile_splits > 1 ? (size_t)total_q * q_heads * d.tile_splits : 0;
+    const size_t places = (size_t)2 * d.single_groups * group, rows = d.tile_split ? (size_t)(d.tiles + tile_more_pieces(c->heads)) * c->heads * AttnTile<128>::ROWS : 0;
     if (places + rows == 0) return d;
     // (the counters first, always of one size: calls of different shapes share a workspace)
     take(COUNTERS);
@@ -118,7 +111,7 @@ int abft_attention(const abft_kv_cache_t* cache, int n_seqs, const int32_t* q_st
     a.c = scale * 1.44269504f;
     a.causal = causal != 0; a.window = window;
     a.single = d.single;
-    a.single_groups = d.single_groups; a.tile_chunk = d.tile_chunk; a.tile_splits = d.tile_splits;
+    a.single_groups = d.single_groups; a.tile_split = d.tile_split;
     a.counters = reinterpret_cast<unsigned*>(ws);
     a.single_o = reinterpret_cast<float*>(ws + d.off_single_o); a.single_ml = reinterpret_cast<float*>(ws + d.off_single_ml);
     a.tile_o = reinterpret_cast<float*>(ws + d.off_tile_o); a.tile_ml = reinterpret_cast<float*>(ws + d.off_tile_ml);

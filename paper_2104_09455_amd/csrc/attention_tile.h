@@ -19,32 +19,72 @@ struct AttnTile {
     static __device__ __forceinline__ int v_swizzle(int r) { return PITCH == 256 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
 };
 
-// which sequence and which of its row tiles the t-th tile of the launch is; false: there is none
-__device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, int& seq, int& tile, int& tiles) {
+// The launch's work: row tiles of each sequence, and pieces of the keys that a row tile sees where splitting them pays.  A piece is
+// `chunk` tiles of keys, counted from the row tile's first, the same for all, so many that the whole work makes about one piece
+// for each workgroup that the chip holds, and at least TILE_MIN_CHUNK (a piece's sums cost as much as three or four tiles);
+// the host cannot know, since lengths are on the device.
+constexpr int TILE_SLOTS = 512, TILE_MIN_CHUNK = 8;
+// (pieces of one head beyond one for each row tile: the sum of keys / chunk over the tiles is at most twice the work in slots)
+constexpr int tile_more_pieces(int heads) { return (2 * TILE_SLOTS + heads - 1) / heads; }
+struct TileWork {
+    int seq, tile, tiles, piece, pieces, chunk, slot;   // slot: index of the piece among all sequences'
+};
+__device__ __forceinline__ int tile_rows(const AttnArgs& p, const SeqInfo& i, int rows) { return p.single && i.nq == 1 ? 0 : (i.nq * p.group + rows - 1) / rows; }
+// tiles of keys that a row tile of the sequence sees, at most
+__device__ __forceinline__ int tile_keys(const AttnArgs& p, const SeqInfo& i, int rows) {
+    const int all = (i.kv + ATTN_BLOCK_KEYS - 1) / ATTN_BLOCK_KEYS;
+    const int seen = p.window > 0 && p.causal ? (min(p.window, i.kv) + rows / p.group + 1) / ATTN_BLOCK_KEYS + 2 : all;
+    return max(min(all, seen), 1);
+}
+// The t-th piece (PIECES) or row tile of the launch; false: there is none.  All of a wavefront.
+template <bool PIECES>
+__device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, TileWork& w) {
     const int lane = threadIdx.x & 63;
-    int before = 0;
-    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
-        const int s = s0 + lane;
-        int n = 0;
-        if (s < p.n_seqs) {
-            const SeqInfo i = seq_info(p, s);
-            if (!(p.single && i.nq == 1)) n = (i.nq * p.group + rows - 1) / rows;
+    int n = 0, keys = 1, mean = 1, chunk = 1 << 30;
+    auto look = [&](int s0) {
+        const SeqInfo i = seq_info(p, min(s0 + lane, p.n_seqs - 1));
+        n = s0 + lane < p.n_seqs ? tile_rows(p, i, rows) : 0;
+        keys = tile_keys(p, i, rows);
+        // (causal without a window: half of the new tokens less, on the average)
+        mean = p.causal && p.window <= 0 ? max(keys - min(i.nq / (2 * ATTN_BLOCK_KEYS), keys / 2), 1) : keys;
+    };
+    if (p.tile_split) {
+        unsigned long long work = 0;
+        for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
+            look(s0);
+            work += (unsigned long long)n * mean;
         }
-        int sum = n;   // of this lane's and all lower ones
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
+        chunk = (int)max((work * p.heads + TILE_SLOTS - 1) / TILE_SLOTS, (unsigned long long)TILE_MIN_CHUNK);
+    }
+    int before = 0, slots = 0;
+    for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
+        if (!p.tile_split || p.n_seqs > 64) look(s0);   // (else it has been)
+        const int pieces = (keys + chunk - 1) / chunk, units = PIECES ? n * pieces : n;
+        int sum = units, slot_sum = n * pieces;   // of this lane's and all lower ones
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(sum, d);
-            if (lane >= d) sum += up;
+            const int up = __shfl_up(sum, d), slot_up = __shfl_up(slot_sum, d);
+            if (lane >= d) {
+                sum += up;
+                slot_sum += slot_up;
+            }
         }
         const unsigned long long at = __ballot(before + sum > t);
         if (at != 0) {
-            const int first = __builtin_ctzll(at);
-            seq = s0 + first;
-            tiles = __shfl(n, first);
-            tile = t - (before + __shfl(sum, first) - tiles);
+            const int first = __builtin_ctzll(at), in = t - (before + readlane(sum, first) - readlane(units, first));
+            w.seq = s0 + first;
+            w.tiles = readlane(n, first);
+            w.pieces = readlane(pieces, first);
+            w.chunk = __builtin_amdgcn_readfirstlane(chunk);
+            w.tile = PIECES ? in / w.pieces : in;
+            w.piece = PIECES ? in - w.tile * w.pieces : 0;
+            w.slot = slots + readlane(slot_sum, first) - w.tiles * w.pieces + w.tile * w.pieces + w.piece;
             return true;
         }
-        before += __shfl(sum, 63);
+        before += readlane(sum, 63);
+        slots += readlane(slot_sum, 63);
     }
     return false;
 }
@@ -88,19 +128,16 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     const int col = lane & 31, h = lane >> 5;   // this lane's row of the wavefront's 32, its half of the keys
 
     const int head = (int)blockIdx.x % p.heads;
-    int seq, tile, tiles;
-    if (!find_tile(p, (int)blockIdx.x / p.heads, T::ROWS, seq, tile, tiles)) return;
-    seq = __builtin_amdgcn_readfirstlane(seq);
-    tile = tiles - 1 - __builtin_amdgcn_readfirstlane(tile);   // (the rows that see most first)
+    TileWork work;
+    if (!find_tile<true>(p, (int)blockIdx.x / p.heads, T::ROWS, work)) return;
+    const int seq = work.seq, tile = work.tiles - 1 - work.tile;   // (the rows that see most first)
     // (what is the workgroup's or the wavefront's goes into scalar registers, or branches and addresses end up in vector code)
     auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     SeqInfo si = seq_info(p, seq);
     si.q0 = scalar(si.q0);
     si.nq = scalar(si.nq);
     si.kv = scalar(si.kv);
-    const int split = blockIdx.y, rows = si.nq * p.group, before = si.kv - si.nq;
-    const int chunks = max(1, (si.kv + p.tile_chunk - 1) / p.tile_chunk);
-    if (split >= chunks) return;
+    const int rows = si.nq * p.group, before = si.kv - si.nq;
 
     // ---- rows: the workgroup's, the wavefront's, this lane's, and the keys that they see, lo .. hi - 1
     auto lo_of = [&](int r) { return p.window > 0 ? max(before + r / p.group - p.window + 1, 0) : 0; };
@@ -111,11 +148,12 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     const int my_row = min(row0 + wave * 32 + col, rows - 1);
     const bool row_on = row0 + wave * 32 + col < rows;
     const int my_lo = lo_of(my_row), my_hi = hi_of(my_row);
-    const int from = max(lo_of(row0), split * p.tile_chunk), to = min(hi_of(row_end), min(si.kv, (split + 1) * p.tile_chunk));
+    const int from = lo_of(row0), to = hi_of(row_end);
     const int full_from = scalar(lo_of(row_end)), full_to = scalar(hi_of(row0));            // keys that all rows of the workgroup see
     const int w_full_from = scalar(lo_of(wrow_end)), w_full_to = scalar(hi_of(wrow0));
-    const int t0 = scalar(from / KEYS), t1 = scalar(to > from ? (to + KEYS - 1) / KEYS : t0);   // tiles of keys
-
+    // tiles of keys: the row tile's, and the piece's
+    const int all0 = from / KEYS, all1 = to > from ? (to + KEYS - 1) / KEYS : all0;
+    const int t0 = scalar(work.piece == 0 ? all0 : min(all0 + work.piece * work.chunk, all1)), t1 = scalar(work.piece == work.pieces - 1 ? all1 : min(t0 + work.chunk, all1));
     // ---- this lane's query, as the fragments of the first product want it: values 16 s + 8 h .. + 7 of its row
     const int token = si.q0 + my_row / p.group, qh = head * p.group + my_row % p.group;
     i32x4 q[STEPS];
@@ -154,6 +192,17 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
 #pragma unroll
             for (int i = 0; i < NP; ++i) key_at[i] = (long long)readlane(lane_key, i);
         }
+    };
+    // LDS addresses: of this lane's part of a fragment of K (step st: with 32 st exclusive-ored in; rows 32 further on have the same
+    // swizzle), of V's (block b: 64 b), and of the thread's widened chunks (the second: 16)
+    const unsigned k_frag = (unsigned)(col * T::PITCH + (h ^ T::k_swizzle(col)) * 16);
+    const int v_row = 4 * h + ((lane & 15) >> 2), v_byte = 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    const unsigned v_frag = (unsigned)(v_row * T::PITCH + (((v_byte >> 4) ^ T::v_swizzle(v_row)) * 16) + (v_byte & 15));
+    const unsigned k_write = (unsigned)(crow * T::PITCH + ((2 * chunk) ^ T::k_swizzle(crow)) * 16), v_write = (unsigned)(crow * T::PITCH + ((2 * chunk) ^ T::v_swizzle(crow)) * 16);
+    // (a copy that the compiler takes for new each time: what is formed from it is not kept over the loop, where registers are short)
+    auto fresh = [](unsigned v) {
+        asm volatile("" : "+v"(v));
+        return v;
     };
     // 16-bit caches: straight into LDS, each lane's chunk from where its place wants it (a chunk of a key beyond the head's values:
     // zeros, since what is not finite would not vanish against the zeros of the queries).
@@ -212,13 +261,12 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     auto finish_k = [&](int stage) {
         if constexpr (I8) {
             char* const ks = k_lds + stage * T::K_STAGE;
+            const unsigned to = fresh(k_write);
 #pragma unroll
             for (int i = 0; i < NP; ++i)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = crow + i * PASS, c = 2 * chunk + e;
-                    *reinterpret_cast<i32x4*>(ks + r * T::PITCH + ((c ^ T::k_swizzle(r)) * 16)) = widen8<DT>(kreg[i][2 * e], kreg[i][2 * e + 1]);
-                }
+                for (int e = 0; e < 2; ++e)
+                    *reinterpret_cast<i32x4*>(ks + i * PASS * T::PITCH + (to ^ (16u * e))) = widen8<DT>(kreg[i][2 * e], kreg[i][2 * e + 1]);
             float* const f = reinterpret_cast<float*>(ks + KEYS * T::PITCH);
             if (lane < NP * PER) {
                 float log2_t, inv_t;
@@ -233,13 +281,12 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     auto finish_v = [&](int kt, int stage) {
         char* const vs = v_lds + stage * T::V_STAGE;
         if constexpr (I8) {
+            const unsigned to = fresh(v_write);
 #pragma unroll
             for (int i = 0; i < NP; ++i)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int r = crow + i * PASS, c = 2 * chunk + e;
-                    *reinterpret_cast<i32x4*>(vs + r * T::PITCH + ((c ^ T::v_swizzle(r)) * 16)) = widen8<DT>(vreg[i][2 * e], vreg[i][2 * e + 1]);
-                }
+                for (int e = 0; e < 2; ++e)
+                    *reinterpret_cast<i32x4*>(vs + i * PASS * T::PITCH + (to ^ (16u * e))) = widen8<DT>(vreg[i][2 * e], vreg[i][2 * e + 1]);
             if (lane < NP * PER) {
                 float log2_t, inv_t;
                 value_scale(vt_reg, log2_t, inv_t);
@@ -285,11 +332,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[kb][r] = 0.f;
 #pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                const int r = kb * 32 + col;
-                const i32x4 a = *reinterpret_cast<const i32x4*>(ks + r * T::PITCH + (((2 * st + h) ^ T::k_swizzle(r)) * 16));
-                s[kb] = MMA::run(a, q[st], s[kb]);
-            }
+            for (int st = 0; st < STEPS; ++st) s[kb] = MMA::run(*reinterpret_cast<const i32x4*>(ks + kb * 32 * T::PITCH + (k_frag ^ (32u * st))), q[st], s[kb]);
         }
     };
     auto scale_scores = [&](int stage, Scores& s) {
@@ -303,6 +346,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
                     const f32x4 lt = *reinterpret_cast<const f32x4*>(fs + KEYS + 32 * kb + 8 * r4);
 #pragma unroll
                     for (int r = 0; r < 4; ++r) s[kb][4 * r4 + r] = __builtin_fmaf(s[kb][4 * r4 + r], kc[r], lt[r]);
+                    if (r4 & 1) __builtin_amdgcn_sched_barrier(0);   // (all of them read at once have no room)
                 }
         }
     };
@@ -341,13 +385,11 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     };
     // a fragment of V^T of the second product: sixteen keys, 32 kb + 16 half + {4 h .. 4 h + 3, 8 + 4 h .. 8 + 4 h + 3}, block b of its values.
     // (Transposing reads: sixteen lanes bring four keys' rows of sixteen values and get a column each.)
-    auto v_fragment = [&](int stage, int kb, int half, int b) {
+    auto v_fragment = [&](int stage, unsigned from, int kb, int half, int b) {
         i32x4 a;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const int r = 32 * kb + 16 * half + 8 * e + 4 * h + ((lane & 15) >> 2);
-            const int byte = 64 * b + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-            const i32x2 v = read_transposed(v_lds + stage * T::V_STAGE + r * T::PITCH + (((byte >> 4) ^ T::v_swizzle(r)) * 16) + (byte & 15));
+            const i32x2 v = read_transposed(v_lds + stage * T::V_STAGE + (32 * kb + 16 * half + 8 * e) * T::PITCH + (from ^ (64u * b)));
             a[2 * e] = v[0];
             a[2 * e + 1] = v[1];
         }
@@ -360,7 +402,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     // matrix instruction (32 cycles) come the next read and about as many cycles of weights.  Left to itself the compiler reads
     // each fragment into the same registers and waits for it.
     auto step = [&](int kt, int stage, Scores& now, Scores& next) {
-        constexpr int NS = 2 * STEPS, NV = 4 * BLOCKS, AHEAD = 6 < NS ? 6 : NS, V_AHEAD = 4;
+        constexpr int NS = 2 * STEPS, NV = 4 * BLOCKS, AHEAD = (I8 ? 4 : 6) < NS ? (I8 ? 4 : 6) : NS, V_AHEAD = I8 ? 3 : 4;   // (int8: no registers for more)
         constexpr int FIRST = 20;   // weights formed beside the scores: at least the first block's, 16 of 32
         const float* const inv_of = reinterpret_cast<const float*>(v_lds + stage * T::V_STAGE + KEYS * T::PITCH) + 4 * h;
         int w[4][4];
@@ -380,9 +422,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
         };
         {
             i32x4 a[AHEAD];
+            const unsigned from = fresh(k_frag);
             auto read = [&](int i) {
-                const int r = (i / STEPS) * 32 + col;
-                a[i % AHEAD] = *reinterpret_cast<const i32x4*>(k_lds + (stage ^ 1) * T::K_STAGE + r * T::PITCH + (((2 * (i % STEPS) + h) ^ T::k_swizzle(r)) * 16));
+                a[i % AHEAD] = *reinterpret_cast<const i32x4*>(k_lds + (stage ^ 1) * T::K_STAGE + (i / STEPS) * 32 * T::PITCH + (from ^ (32u * (i % STEPS))));
             };
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) read(i);
@@ -404,7 +446,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
             }
         }
         i32x4 a[V_AHEAD];
-        auto read = [&](int i) { a[i % V_AHEAD] = v_fragment(stage, i / (2 * BLOCKS), i / BLOCKS % 2, i % BLOCKS); };
+        const unsigned from = fresh(v_frag);
+        auto read = [&](int i) { a[i % V_AHEAD] = v_fragment(stage, from, i / (2 * BLOCKS), i / BLOCKS % 2, i % BLOCKS); };
 #pragma unroll
         for (int i = 0; i < V_AHEAD; ++i) read(i);
         if constexpr (!I8) mask_scores(kt + 1, next);
@@ -485,7 +528,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     // ---- out: this lane's row, values 32 b + 8 (r / 4) + 4 h + r % 4
     l += swap_halves(l);
     if (!row_on) return;
-    if (chunks == 1) {
+    if (work.pieces == 1) {
         const float inv = l == 0.f ? 0.f : 1.f / l;
         char* const dst = p.O + (token * p.ldo + (long long)qh * p.dim) * 2;
 #pragma unroll
@@ -499,8 +542,10 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
                 if (d < p.dim) *reinterpret_cast<i32x2*>(dst + 2 * d) = v;
             }
     } else {
-        const long long at = ((long long)token * p.heads * p.group + qh) * p.tile_splits + split;
-        float* const dst = p.tile_o + at * p.dim;
+        const long long place = ((long long)work.slot * p.heads + head) * T::ROWS + wave * 32 + col;
+        float* const dst = p.tile_o + place * p.dim;
+        if (h == 0) *reinterpret_cast<float2*>(p.tile_ml + 2 * place) = float2{m, l};
+        if (t1 == t0) return;   // (no weights: the sums are not read)
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
@@ -508,30 +553,62 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
                 const int d = 32 * b + 2 * r + 4 * h;
                 if (d < p.dim) *reinterpret_cast<f32x4*>(dst + d) = f32x4{o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]};
             }
-        if (h == 0) {
-            p.tile_ml[2 * at] = m;
-            p.tile_ml[2 * at + 1] = l;
-        }
     }
 }
 
-// The splits of a row put together, a wavefront per row.
+// The pieces of rows put together: eight lanes a row, four workgroups a row tile and head.
 template <int DT>
 __global__ __launch_bounds__(256) void attn_tile_join_kernel(const AttnArgs p) {
-    const int qheads = p.heads * p.group;
-    const long long row = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    if (row >= (long long)p.total_q * qheads) return;
-    const int token = (int)(row / qheads), qh = (int)(row - (long long)token * qheads);
-    int a = 0, b = p.n_seqs;   // the last sequence that starts at or before the token
-    while (b - a > 1) {
-        const int mid = (a + b) / 2;
-        if (p.q_start[mid] <= token) a = mid;
-        else b = mid;
+    constexpr int ROWS = AttnTile<128>::ROWS;
+    const int head = (int)blockIdx.x % p.heads, quarter = (int)blockIdx.x / p.heads % 4;
+    TileWork work;
+    if (!find_tile<false>(p, (int)blockIdx.x / p.heads / 4, ROWS, work)) return;
+    if (work.pieces == 1) return;
+    const SeqInfo si = seq_info(p, work.seq);
+    const int in_tile = quarter * 32 + (int)threadIdx.x / 8, row = (work.tiles - 1 - work.tile) * ROWS + in_tile;
+    if (row >= si.nq * p.group) return;
+    // sixteen values a lane, four in a row out of every 32
+    const int part = (threadIdx.x & 7) * 4;
+    float M = ATTN_NONE, L = 0.f;
+    f32x4 acc[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const long long place = ((long long)work.slot * p.heads + head) * ROWS + in_tile, step = (long long)p.heads * ROWS;
+    for (int i0 = 0; i0 < work.pieces; i0 += 4) {
+        // four pieces on their way at a time
+        float2 ml[4];
+        f32x4 x[4][4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const long long at = place + min(i0 + u, work.pieces - 1) * step;
+            ml[u] = *reinterpret_cast<const float2*>(p.tile_ml + 2 * at);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[u][c] = *reinterpret_cast<const f32x4*>(p.tile_o + at * p.dim + (32 * c + part < p.dim ? 32 * c + part : 0));
+        }
+        const float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(ml[0].x, ml[1].x), __builtin_fmaxf(ml[2].x, ml[3].x)), M);
+        const float f0 = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        L *= f0;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] *= f0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (i0 + u >= work.pieces || ml[u].y == 0.f) continue;
+            const float f = __builtin_amdgcn_exp2f(ml[u].x - M);
+            L = __builtin_fmaf(f, ml[u].y, L);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[c][e] = __builtin_fmaf(f, x[u][c][e], acc[c][e]);
+        }
     }
-    const SeqInfo si = seq_info(p, a);
-    if (token < si.q0 || token >= si.q0 + si.nq || (p.single && si.nq == 1)) return;
-    const int n = (si.kv + p.tile_chunk - 1) / p.tile_chunk;
-    if (n > 1) attn_join_row<DT>(p, n, [&](int i) { return row * p.tile_splits + i; }, p.tile_o, p.tile_ml, token, qh);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const int token = si.q0 + row / p.group, qh = head * p.group + row % p.group;
+    char* const dst = p.O + (token * p.ldo + (long long)qh * p.dim) * 2;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+        if (32 * c + part < p.dim)
+            *reinterpret_cast<i32x2*>(dst + 2 * (32 * c + part)) = i32x2{pack_out16<DT>(acc[c][0] * inv, acc[c][1] * inv), pack_out16<DT>(acc[c][2] * inv, acc[c][3] * inv)};
 }
 
 }  // namespace abft
