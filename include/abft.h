@@ -452,18 +452,23 @@ int abft_quantize_rows(int M, int K, const void *X, int64_t ldx, int dtype, void
  *   row_scale: M floats (abft_quantize_rows); col_scale: N floats; bias: N floats or NULL.
  *   act: abft_act_t.  C: M x N, ldc >= N, of type out_dtype (F16 / BF16).  C[m][n] is the sum as a float, times row_scale[m], times
  *       col_scale[n] plus bias[n] in one fused step, after the activation function, rounded once to nearest even.
- *   mode: ABFT_NONE, ABFT_GLOBAL, ABFT_THREAD, or ABFT_AUTO (abft_select for ABFT_I8); the others: ABFT_E_UNSUPPORTED.
+ *   mode: ABFT_NONE, ABFT_GLOBAL, ABFT_THREAD, or ABFT_AUTO (abft_scaled_select); the others: ABFT_E_UNSUPPORTED.
  *   K: at most 131071 (the sums stay within int32), else ABFT_E_SHAPE. */
 int abft_gemm_scaled(int M, int N, int K, const void *A, int64_t lda, const float *row_scale, const void *B, int64_t ldb,
                      int b_layout, const float *col_scale, const float *bias, int act, void *C, int64_t ldc, int out_dtype,
                      int mode, const void *beta, void *workspace, size_t workspace_bytes, uint32_t *fault_flag,
                      abft_report_t *report, const abft_fault_t *inject, void *stream);
 
+/* The scheme that ABFT_AUTO stands for in these calls: the faster protected one by measurement (`aligned` as for abft_region_shape).
+ * ABFT_THREAD or ABFT_GLOBAL, or a negative error. */
+int abft_scaled_select(int M, int N, int K, int aligned);
+
 /* The two in one call: a linear layer of 16-bit activations X (M x K, ldx >= K, F16 / BF16) and int8 weights B with a
  * scale per output channel; C has the type of X.  The quantised activations and their scales live in the workspace (256-byte
  * aligned, abft_linear_scaled_workspace_bytes bytes, whatever the mode; no initialisation), in rows padded to whole
  * chunks: `aligned` of abft_region_shape is K % 16 == 0 and an aligned B in ABFT_B_NK order.  Results are those of
- * abft_quantize_rows and abft_gemm_scaled.  What is refused is refused before anything is launched. */
+ * abft_quantize_rows and abft_gemm_scaled, bit for bit.  (Up to four rows may be quantised inside the product's kernel: one launch.)
+ * What is refused is refused before anything is launched. */
 int abft_linear_scaled(int M, int N, int K, const void *X, int64_t ldx, int dtype, const void *B, int64_t ldb, int b_layout,
                        const float *col_scale, const float *bias, int act, void *C, int64_t ldc, int mode, const void *beta,
                        void *workspace, size_t workspace_bytes, uint32_t *fault_flag, abft_report_t *report,

@@ -67,7 +67,7 @@ EXPORTS = [
     "abft_plan_set_activation", "abft_plan_activation", "abft_gemm_static", "abft_static_scratch_bytes",
     "abft_tolerance_half_coeff", "abft_plan_run_chain", "abft_plan_chain_status", "abft_plan_chain_reset",
     "abft_plan_set_diagnostics", "abft_kernel_name", "abft_handover_launches", "abft_chain_launches", "abft_shared_launches", "abft_mfma_probe", "abft_mfma_probe_bytes",
-    "abft_quantize_rows", "abft_gemm_scaled", "abft_linear_scaled", "abft_linear_scaled_workspace_bytes",
+    "abft_quantize_rows", "abft_gemm_scaled", "abft_linear_scaled", "abft_linear_scaled_workspace_bytes", "abft_scaled_select",
     "abft_kv_write", "abft_kv_read", "abft_attention", "abft_attention_workspace_bytes",
 ]
 
@@ -181,6 +181,8 @@ def lib() -> ctypes.CDLL:
                                      ctypes.POINTER(Fault), vp]
     L.abft_linear_scaled_workspace_bytes.restype = sz
     L.abft_linear_scaled_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    L.abft_scaled_select.restype = ci
+    L.abft_scaled_select.argtypes = [ci, ci, ci, ci]
     cp = ctypes.POINTER(KVCache)
     for f in (L.abft_kv_write, L.abft_kv_read):
         f.restype = ci
@@ -474,6 +476,13 @@ def abft_linear_scaled(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias
     _check(lib().abft_linear_scaled(M, N, K, _ptr(X), ldx, dtype, _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act, _ptr(C),
                                     ldc, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag), _ptr(report), ip,
                                     _stream(stream)))
+
+
+def abft_scaled_select(M, N, K, aligned=True) -> int:
+    rc = lib().abft_scaled_select(M, N, K, 1 if aligned else 0)
+    if rc < 0:
+        raise AbftError(rc)
+    return rc
 
 
 def abft_linear_scaled_workspace_bytes(M, N, K, mode) -> int:

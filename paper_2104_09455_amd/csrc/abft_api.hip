@@ -829,6 +829,15 @@ double intensity(int M, int N, int K, int dt) {
 int select_mode(int M, int N, int K, int dt) {
     return intensity(M, N, K, dt) > cmr_of(dt) ? ABFT_GLOBAL : ABFT_THREAD;
 }
+// The faster protected scheme of a scaled product.  Aligned, the global one wherever 32 x 32 tiles are more than one per compute unit:
+// beyond that the thread-level one forms its checksums on the vector unit of every wavefront (bf16 out, thread-level / global,
+// us: 64 x 4096 x 4096 7.7 / 8.2, 96 rows 13.1 / 9.4, 256 rows 17.3 / 12.4, 1024 46 / 26; 128 x 2048 x 8192 9.9 / 10.7, 192 rows
+// 20.3 / 13.2; 512 x 512 x 512 4.3 / 4.5, 1024 rows 5.7 / 5.1).  Else the global one takes a pass over A, and the intensity decides as
+// ever (511 x 1000 x 2047 9.7 / 17.8).
+int scaled_select(int M, int N, int K, bool aligned) {
+    if (aligned) return cdiv(M, 32) * cdiv(N, 32) > 256 ? ABFT_GLOBAL : ABFT_THREAD;
+    return select_mode(M, N, K, ABFT_I8);
+}
 
 hipError_t launch_weight_checksum(int K, int N, const void* B, long long ldb, int layout, int dt, int block_n,
                                   void* beta_buf, hipStream_t st) {
@@ -1013,9 +1022,9 @@ hipError_t quantize_rows(int M, int K, const void* X, long long ldx, int dtype, 
     a.M = M; a.K = K; a.ldx = ldx; a.ldq = ldq;
     return dtype == ABFT_F16 ? launch_quantize_rows<DT_F16>(a, st) : launch_quantize_rows<DT_BF16>(a, st);
 }
-// A scaled product as a problem, checked as far as it is more than one in int8.  K: beyond it 128 * 128 * K passes an int32.
+// A scaled product as a problem, checked as far as it is more than one in int8; AUTO becomes a scheme.  K: beyond it 128 * 128 * K passes an int32.
 int scaled_problem(int M, int N, int K, const void* A, long long lda, const float* row_scale, const void* B, long long ldb, int b_layout,
-                   const float* col_scale, const float* bias, int act, void* C, long long ldc, int out_dtype, int mode, const uint32_t* flag,
+                   const float* col_scale, const float* bias, int act, void* C, long long ldc, int out_dtype, int& mode, const uint32_t* flag,
                    Problem& pr) {
     std::memset(&pr, 0, sizeof pr);
     pr.M = M; pr.N = N; pr.K = K; pr.dtype = ABFT_I8; pr.b_layout = b_layout;
@@ -1028,7 +1037,8 @@ int scaled_problem(int M, int N, int K, const void* A, long long lda, const floa
     if (K > SCALED_MAX_K) return ABFT_E_SHAPE;
     const int rc = validate_common(pr, mode, flag);
     if (rc != ABFT_OK) return rc;
-    return mode == ABFT_NONE || mode == ABFT_GLOBAL || mode == ABFT_THREAD || mode == ABFT_AUTO ? ABFT_OK : ABFT_E_UNSUPPORTED;
+    if (mode == ABFT_AUTO) mode = scaled_select(M, N, K, a_vectorisable(pr) && b_vectorisable(pr));
+    return mode == ABFT_NONE || mode == ABFT_GLOBAL || mode == ABFT_THREAD ? ABFT_OK : ABFT_E_UNSUPPORTED;
 }
 // where a linear layer's workspace holds the quantised activations (rows of whole 16-byte chunks, at its start), their scales, and
 // what the product wants
@@ -1489,8 +1499,15 @@ int abft_gemm_scaled(int M, int N, int K, const void* A, int64_t lda, const floa
     return run_problem(pr, mode, beta, workspace, workspace_bytes, fault_flag, report, inject, reinterpret_cast<hipStream_t>(stream));
 }
 
+int abft_scaled_select(int M, int N, int K, int aligned) {
+    if (M <= 0 || N <= 0 || K <= 0) return ABFT_E_SHAPE;
+    return scaled_select(M, N, K, aligned != 0);
+}
+
 size_t abft_linear_scaled_workspace_bytes(int M, int N, int K, int mode) {
     if (M <= 0 || N <= 0 || K <= 0) return 0;
+    // (whatever the alignment will be)
+    if (mode == ABFT_AUTO) mode = scaled_select(M, N, K, true) == ABFT_GLOBAL ? ABFT_GLOBAL : scaled_select(M, N, K, false);
     return linear_product_offset(M, K) + plain_workspace_bytes(M, N, K, ABFT_I8, mode);
 }
 
@@ -1512,6 +1529,18 @@ int abft_linear_scaled(int M, int N, int K, const void* X, int64_t ldx, int dtyp
     const size_t left = workspace_bytes - product;
     if (left < plain_workspace_bytes(M, N, K, ABFT_I8, mode)) return ABFT_E_WORKSPACE;
     if (inject && !inject_in_range(pr, mode, *inject)) return ABFT_E_INJECT;
+    if (skinny_few_fits(M, K) && mode != ABFT_GLOBAL && !report && !inject) {
+        // one launch where the product's kernel can quantise the few rows itself
+        Prepared w;
+        rc = prepare_problem(pr, mode, nullptr, nullptr, 0, fault_flag, nullptr, nullptr, st, w);
+        if (rc != ABFT_OK) return rc;
+        if (w.skinny) {
+            const bool bytes = rows_off_dwords(w.g, ABFT_I8);
+            w.g.A = reinterpret_cast<const char*>(X);
+            w.g.lda = ldx;
+            return (dtype == ABFT_F16 ? launch_scaled_few_f16 : launch_scaled_few_bf16)(w.kmode, bytes, w.g, st) == hipSuccess ? ABFT_OK : ABFT_E_HIP;
+        }
+    }
     if (quantize_rows(M, K, X, ldx, dtype, ws, linear_ld(K), row_scale, st) != hipSuccess) return ABFT_E_HIP;
     return run_problem(pr, mode, beta, left ? ws + product : nullptr, left, fault_flag, report, inject, st);
 }

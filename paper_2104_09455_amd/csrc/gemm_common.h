@@ -270,6 +270,15 @@ __device__ __forceinline__ T wave_sum(T v) {
     return (a + b) + (c + d);
 }
 
+// the largest over the 64 lanes, in every lane
+__device__ __forceinline__ unsigned wave_max(unsigned v) {
+    v = max(v, dpp_move<0xB1>(v));
+    v = max(v, dpp_move<0x4E>(v));
+    v = max(v, dpp_move<0x141>(v));
+    v = max(v, dpp_move<0x140>(v));
+    return max(max(readlane(v, 0), readlane(v, 16)), max(readlane(v, 32), readlane(v, 48)));
+}
+
 // ---------------------------------------------------------------------------
 // Tile configuration
 // ---------------------------------------------------------------------------

@@ -142,6 +142,7 @@ ABFT_DECLARE_LAUNCHES(i8)
     hipError_t launch_scaled_stream_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);  \
     hipError_t launch_scaled_generic_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream); \
     hipError_t launch_scaled_skinny_##out(int mode, bool bytes, int columns, const GemmArgs& args, hipStream_t stream); \
+    hipError_t launch_scaled_few_##out(int mode, bool bytes, const GemmArgs& args, hipStream_t stream);                  \
     inline hipError_t launch_scaled_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream) {   \
         if (cfg_is_stream(cfg)) return launch_scaled_stream_##out(cfg, mode, inject, args, stream);                  \
         if (cfg_is_generic(cfg)) return launch_scaled_generic_##out(cfg, mode, inject, args, stream);                \

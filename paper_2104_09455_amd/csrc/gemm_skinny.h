@@ -17,7 +17,7 @@
 // Bound: the latency of one round trip to the weights, then the weights' bytes and A's (as many again, from L2: 16 x
 // 4096 x 4096 takes 8.0 without them).
 #pragma once
-#include "gemm_common.h"
+#include "quantize.h"
 
 namespace abft {
 
@@ -29,7 +29,17 @@ constexpr int skinny_lds_bytes(int tn) { return SKINNY_WAVES * (1 + tn) * 2048; 
 // hook): in the sum of those of the eight shares that the tiling whose place this kernel takes has in one (p.n_parts shares, k tile t in
 // share t % p.n_parts), as it stands once that share has taken all its k tiles up to p.f_kt (-1: up to the last), or in the finished sum (-2).
 // The loop and the comparison are those of a call without one, and so is every other element.
-template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT>
+// FEW (scaled products): at most SKINNY_FEW rows of A are not there yet: p.A holds 16-bit activations of type OUT, and each workgroup
+// quantises them for itself, into LDS, while its first weights are on their way.  (A launch of its own takes 2.3 us and a
+// gap; sixteen rows read by every workgroup would take longer than that.)
+constexpr int SKINNY_FEW = 4, SKINNY_FEW_BYTES = 32 * 1024;
+constexpr int skinny_few_bytes(int rows, int k) { return (k + 127) / 128 * 128 * rows; }   // quantised, in LDS
+// whether a workgroup's threads can hold such rows: eight chunks of eight values each, a row's in as many as it needs
+constexpr bool skinny_few_fits(int rows, int k) {
+    return rows <= SKINNY_FEW && rows * ((skinny_few_bytes(1, k) + 64 * SKINNY_WAVES * 8 - 1) / (64 * SKINNY_WAVES * 8)) <= SKINNY_FEW_BYTES / (64 * SKINNY_WAVES * 8);
+}
+
+template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT, bool FEW = false>
 __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char* smem) {
     typedef Mma<DT, 16> MMA;
     typedef typename MMA::Acc Acc;
@@ -50,9 +60,11 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
     constexpr bool SCALED = OUT != DT;
     f32x4 row_scale;
     float col_scale, col_bias;
+    static_assert(!FEW || (SCALED && !INJ), "quantised on the way");
+    constexpr int Q0 = FEW ? 2 : 0;   // (blocks of A are not copied then)
     if constexpr (SCALED) {
         const int n = min(n0 + 16 * (TN == 1 ? 0 : wave & 1) + lrow, N - 1);
-        row_scale = row_scales(p, 4 * lgrp);
+        if constexpr (!FEW) row_scale = row_scales(p, 4 * lgrp);
         col_scale = p.col_scale[n];
         col_bias = p.bias ? p.bias[n] : 0.f;
     }
@@ -67,7 +79,7 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
     const char* row[NQ];
     bool in[NQ];
 #pragma unroll
-    for (int q = 0; q < NQ; ++q) {
+    for (int q = Q0; q < NQ; ++q) {
         const int r = (q & 1) * 8 + crow, n = n0 + (q >> 1) * 16 - 16 + r;
         in[q] = q < 2 ? r < M : n < N;   // (rows outside read zeros and stay there)
         row[q] = !in[q] ? g_zero_chunk : q < 2 ? p.A + (long long)r * p.lda * ES : p.B + (long long)n * p.ldb * ES;
@@ -90,7 +102,7 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
     auto load_whole = [&](int u, int i) {
         const int off = (wave + KW * i) * 128 + chunk;
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) fetch(u, q, row[q] + (in[q] ? off : 0));
+        for (int q = Q0; q < NQ; ++q) fetch(u, q, row[q] + (in[q] ? off : 0));
     };
     auto load = [&](int u, int i) {
         const int t = wave + KW * i;
@@ -99,7 +111,7 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
         } else {
             const int off = t * 128 + chunk, from = off + 16 > kb ? kb - 16 : off;
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) fetch(u, q, in[q] && off < kb ? row[q] + from : g_zero_chunk);
+            for (int q = Q0; q < NQ; ++q) fetch(u, q, in[q] && off < kb ? row[q] + from : g_zero_chunk);
         }
     };
     const int kx = (crow >> 1) * 16;   // (rows 8 further on: the key's top bit)
@@ -124,9 +136,12 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
 #pragma unroll
         for (int j = 0; j < TN; ++j) then[j] = acc[j];
     }
+    // FEW: row r's chunk c of k tile t at r * row bytes + 128 t + 16 (c ^ r); other rows' fragments are zeros
+    char* const few = smem + skinny_lds_bytes(TN);
+    const int few_at = lrow < M ? lrow * (nkt * 128) + (lgrp ^ lrow) * 16 : 0;
     auto multiply = [&](int u, int i, int cut) {
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
+        for (int q = Q0; q < NQ; ++q) {
             i32x4 x = v_[u][q];
             if constexpr (BYTES) {
 #pragma unroll
@@ -138,7 +153,13 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const i32x4 a = *reinterpret_cast<const i32x4*>(own + at[s]);
+            i32x4 a;
+            if constexpr (FEW) {
+                a = *reinterpret_cast<const i32x4*>(few + ((wave + KW * i) * 128 + (few_at ^ (64 * s))));
+                if (lrow >= M) a = i32x4{0, 0, 0, 0};
+            } else {
+                a = *reinterpret_cast<const i32x4*>(own + at[s]);
+            }
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
                 const i32x4 b = *reinterpret_cast<const i32x4*>(own + (1 + j) * 2048 + at[s]);
@@ -153,11 +174,51 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
             }
         }
     };
+    // FEW: the rows quantised (eight threads' reads of a row are whole lines); only then does anything multiply
+    auto quantise_rows = [&]() {
+        if constexpr (FEW) {
+            unsigned* const tops = reinterpret_cast<unsigned*>(smem);   // (the fragments' place, not in use yet)
+            if (tid < SKINNY_FEW) tops[tid] = 0;
+            __syncthreads();
+            // chunks of eight values: a row has `per` for each thread, and all rows at most HELD
+            constexpr int HELD = SKINNY_FEW_BYTES / (64 * KW * 8);
+            const int per = (nkt * 128 + 64 * KW * 8 - 1) / (64 * KW * 8);
+            i32x4 v[HELD];
+            auto at_k = [&](int c) { return (c % per * 64 * KW + tid) * 8; };
+#pragma unroll
+            for (int c = 0; c < HELD; ++c) v[c] = c / per < M && at_k(c) < K ? row_chunk16(p.A + (long long)(c / per) * p.lda * 2, at_k(c), K) : i32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < HELD; ++c) {
+                if (c / per >= M) break;
+                const unsigned top = (unsigned)chunk_magnitude(v[c], 0), best = wave_max(max(top & 0xffffu, top >> 16));
+                if (lane == 0) atomicMax(&tops[c / per], best);
+            }
+            __syncthreads();
+            GroupScale g[SKINNY_FEW];
+#pragma unroll
+            for (int r = 0; r < SKINNY_FEW; ++r) {
+                g[r] = group_scale<OUT>(tops[r]);
+                row_scale[r] = g[r].scale;   // (of rows 4 lgrp + r those of the first lanes are used)
+            }
+            __syncthreads();   // (the wavefronts' own places from here on)
+#pragma unroll
+            for (int c = 0; c < HELD; ++c) {
+                const int r = c / per, k = at_k(c), piece = k >> 4;
+                if (r >= M) break;
+                const GroupScale& gr = r == 0 ? g[0] : r == 1 ? g[1] : r == 2 ? g[2] : g[3];
+                // (zeros behind the row's end, as far as its last k tile goes)
+                if (k < nkt * 128)
+                    *reinterpret_cast<i32x2*>(few + r * (nkt * 128) + (piece >> 3) * 128 + ((piece & 7) ^ r) * 16 + (k & 8)) = quantize_chunk<OUT>(v[c], gr);
+            }
+            __syncthreads();
+        }
+    };
     int i = 0;
     if (n_own > 2 * U) {
         // (no condition between the loads, so that the number behind the one that is waited for is known)
 #pragma unroll
         for (int u = 0; u < U; ++u) load_whole(u, u);
+        quantise_rows();
 #pragma nounroll
         for (; i + 2 * U < n_own; i += U)
 #pragma unroll
@@ -169,6 +230,7 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u < n_own) load(u, u);
+        quantise_rows();
     }
 #pragma nounroll
     for (; i < n_own; i += U)
@@ -288,12 +350,12 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
     }
 }
 
-template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT>
+template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT, bool FEW = false>
 __global__ __launch_bounds__(64 * SKINNY_WAVES) void gemm_skinny_kernel(const GemmArgs p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     int tile_m, tile_n;
     tile_of_block((int)blockIdx.x, 1, (int)gridDim.x, tile_m, tile_n);   // (a run of columns per die: whole lines of C and A once)
-    skinny_tile<DT, TN, MODE, BYTES, INJ, OUT>(p, tile_n, smem);
+    skinny_tile<DT, TN, MODE, BYTES, INJ, OUT, FEW>(p, tile_n, smem);
 }
 
 }  // namespace abft

@@ -123,8 +123,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs p
         for (long long k = t * 8; k < K; k += TPR * 8) top = chunk_magnitude(row_chunk16(row, (int)k, K), top);
     }
     unsigned best = max((unsigned)top & 0xffffu, (unsigned)top >> 16);
-#pragma unroll
-    for (int s = 1; s < 64; s <<= 1) best = max(best, (unsigned)__shfl_xor((int)best, s));
+    best = wave_max(best);
     if constexpr (TPR == 256) {
         if ((tid & 63) == 0) tops[tid >> 6] = best;
         __syncthreads();

@@ -78,6 +78,16 @@ def test_linear_workspace():
     assert B.abft_linear_scaled_workspace_bytes(0, 8, 8, B.NONE) == 0
 
 
+def test_scheme_of_scaled_products():
+    """Aligned: the tiles of 32 x 32 against the compute units; else the rule of plain products."""
+    assert B.abft_scaled_select(64, 4096, 4096) == B.THREAD
+    assert B.abft_scaled_select(65, 4096, 4096) == B.GLOBAL
+    assert B.abft_scaled_select(8192, 32, 64) == B.THREAD
+    for M, N, K in ((500, 1000, 2047), (8192, 8192, 8191)):
+        assert B.abft_scaled_select(M, N, K, aligned=False) == B.abft_select(M, N, K, B.I8)
+    refuses(E_SHAPE, lambda: B.abft_scaled_select(0, 1, 1))
+
+
 CACHE = dict(k=P, v=P, k_scale=P, v_scale=P, dtype=B.I8, pages=4, page_size=16, heads=2, head_dim=64)
 BAD_CACHES = [(dict(k=None), E_NULL), (dict(v=None), E_NULL), (dict(k_scale=None), E_NULL), (dict(v_scale=None), E_NULL), (dict(k=P + 8), E_LD), (dict(v_scale=P + 4), E_LD),
               (dict(dtype=B.BF16), E_ENUM), (dict(dtype=5), E_ENUM), (dict(pages=0), E_SHAPE), (dict(heads=0), E_SHAPE), (dict(head_dim=24), E_SHAPE),

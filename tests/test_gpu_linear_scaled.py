@@ -123,7 +123,7 @@ class Product:
         self.C.fill_(55.0)
         self.flag.zero_()
         self.rep.zero_()
-        n = B.abft_workspace_bytes(self.M, self.N, self.K, B.I8, mode)
+        n = B.abft_workspace_bytes(self.M, self.N, self.K, B.I8, B.abft_scaled_select(self.M, self.N, self.K, self.aligned) if mode == B.AUTO else mode)
         ws = torch.full((n,), 201, dtype=torch.uint8, device=DEV) if n else None
         beta = None
         if with_beta:
@@ -204,7 +204,8 @@ def test_scales_that_are_nan_or_zero():
 
 @pytest.mark.parametrize("mode", [B.NONE, B.GLOBAL, B.THREAD, B.AUTO])
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("M,N,K,layout", [(1, 96, 64, B.B_NK), (1, 33, 7, B.B_KN), (16, 512, 4100, B.B_NK), (9, 4096, 2048, B.B_NK), (130, 200, 300, B.B_NK), (600, 1030, 512, B.B_NK)])
+@pytest.mark.parametrize("M,N,K,layout", [(1, 96, 64, B.B_NK), (1, 33, 7, B.B_KN), (1, 1, 17, B.B_NK), (2, 40, 130, B.B_NK), (3, 100, 1001, B.B_NK), (4, 4096, 8192, B.B_NK), (4, 50, 8193, B.B_NK), (1, 70, 32768, B.B_NK),
+                                      (3, 16, 10000, B.B_NK), (5, 64, 256, B.B_NK), (16, 512, 4100, B.B_NK), (9, 4096, 2048, B.B_NK), (130, 200, 300, B.B_NK), (600, 1030, 512, B.B_NK)])
 def test_linear_layer_is_its_two_steps(M, N, K, layout, dtype, mode):
     """Bit for bit what the quantisation and the scaled product give, on a stream of its own."""
     p = Product(M, N, K, dtype, layout, seed=K)
@@ -229,6 +230,28 @@ def test_linear_layer_is_its_two_steps(M, N, K, layout, dtype, mode):
     side.synchronize()
     assert int(p.flag.item()) == 0
     assert torch.equal(out.view(torch.int16), want.contiguous().view(torch.int16))
+
+
+@pytest.mark.parametrize("M", [1, 4])
+def test_few_rows_with_a_report_or_a_planted_fault(M):
+    """Calls that cannot take the few rows' kernel give its results, and see a fault."""
+    p = Product(M, 200, 520, "f16", B.B_NK, seed=M)
+    x = hard_rows(M, 520, p.t, seed=2)
+    n = B.abft_linear_scaled_workspace_bytes(M, 200, 520, B.THREAD)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    outs = []
+    for report, inject in ((None, None), (p.rep, None), (None, B.Fault(M - 1, 77, 20, -1))):
+        out = torch.empty(M, 200, dtype=p.t, device=DEV)
+        p.flag.zero_()
+        B.abft_linear_scaled(M, 200, 520, x, 520, p.dt, p.Bm, p.ldb, B.B_NK, p.cs, p.bias, B.ACT_NONE, out, 200, B.THREAD, workspace=ws, workspace_bytes=n,
+                             fault_flag=p.flag, report=report, inject=inject)
+        torch.cuda.synchronize()
+        assert int(p.flag.item()) == (1 if inject else 0)
+        outs.append(out.view(torch.int16).clone())
+    assert torch.equal(outs[0], outs[1])
+    differs = outs[0] != outs[2]
+    differs[M - 1, 77] = False
+    assert not differs.any()
 
 
 def test_linear_layer_in_a_graph():
