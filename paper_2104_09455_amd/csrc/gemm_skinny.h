@@ -30,14 +30,14 @@ constexpr int skinny_lds_bytes(int tn) { return SKINNY_WAVES * (1 + tn) * 2048; 
 // share t % p.n_parts), as it stands once that share has taken all its k tiles up to p.f_kt (-1: up to the last), or in the finished sum (-2).
 // The loop and the comparison are those of a call without one, and so is every other element.
 // FEW (scaled products): at most SKINNY_FEW rows of A are not there yet: p.A holds 16-bit activations of type OUT, and each workgroup
-// quantises them for itself, into LDS, while its first weights are on their way.  (A launch of its own takes 2.3 us and a
-// gap; sixteen rows read by every workgroup would take longer than that.)
-constexpr int SKINNY_FEW = 4, SKINNY_FEW_BYTES = 32 * 1024;
+// quantises them for itself, into LDS, while its first weights are on their way.  (Quantised by
+// a launch of their own / here, microseconds per call: 1 x 4096 x 4096 6.95 / 5.2, 2 rows 7.0 / 5.6, 4 rows 7.1 / 6.6, 2 x 4096 x 8192 9.5 / 7.9.
+// Rows past four chunks a thread are level, 4 x 4096 x 8192 9.9 / 9.7, and have a launch of their own.)
+constexpr int SKINNY_FEW = 4, SKINNY_FEW_BYTES = 16 * 1024;
 constexpr int skinny_few_bytes(int rows, int k) { return (k + 127) / 128 * 128 * rows; }   // quantised, in LDS
-// whether a workgroup's threads can hold such rows: eight chunks of eight values each, a row's in as many as it needs
-constexpr bool skinny_few_fits(int rows, int k) {
-    return rows <= SKINNY_FEW && rows * ((skinny_few_bytes(1, k) + 64 * SKINNY_WAVES * 8 - 1) / (64 * SKINNY_WAVES * 8)) <= SKINNY_FEW_BYTES / (64 * SKINNY_WAVES * 8);
-}
+// A thread holds four chunks of eight values, 2^lg of each row; whether that is enough for these rows
+constexpr int skinny_few_lg(int k) { return k <= 4096 ? 0 : k <= 8192 ? 1 : 2; }
+constexpr bool skinny_few_fits(int rows, int k) { return rows <= SKINNY_FEW && k <= 16384 && (rows << skinny_few_lg(k)) <= 4; }
 
 template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT, bool FEW = false>
 __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char* smem) {
@@ -180,18 +180,21 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
             unsigned* const tops = reinterpret_cast<unsigned*>(smem);   // (the fragments' place, not in use yet)
             if (tid < SKINNY_FEW) tops[tid] = 0;
             __syncthreads();
-            // chunks of eight values: a row has `per` for each thread, and all rows at most HELD
+            // chunks of eight values: a row has 2^lg for each thread, and all rows at most HELD
             constexpr int HELD = SKINNY_FEW_BYTES / (64 * KW * 8);
-            const int per = (nkt * 128 + 64 * KW * 8 - 1) / (64 * KW * 8);
+            const int lg = skinny_few_lg(K);
             i32x4 v[HELD];
-            auto at_k = [&](int c) { return (c % per * 64 * KW + tid) * 8; };
-#pragma unroll
-            for (int c = 0; c < HELD; ++c) v[c] = c / per < M && at_k(c) < K ? row_chunk16(p.A + (long long)(c / per) * p.lda * 2, at_k(c), K) : i32x4{0, 0, 0, 0};
+            auto at_k = [&](int c) { return ((c & ((1 << lg) - 1)) * 64 * KW + tid) * 8; };
 #pragma unroll
             for (int c = 0; c < HELD; ++c) {
-                if (c / per >= M) break;
+                if ((c >> lg) >= M) break;
+                v[c] = at_k(c) < K ? row_chunk16(p.A + (long long)(c >> lg) * p.lda * 2, at_k(c), K) : i32x4{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int c = 0; c < HELD; ++c) {
+                if ((c >> lg) >= M) break;
                 const unsigned top = (unsigned)chunk_magnitude(v[c], 0), best = wave_max(max(top & 0xffffu, top >> 16));
-                if (lane == 0) atomicMax(&tops[c / per], best);
+                if (lane == 0) atomicMax(&tops[c >> lg], best);
             }
             __syncthreads();
             GroupScale g[SKINNY_FEW];
@@ -203,9 +206,15 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
             __syncthreads();   // (the wavefronts' own places from here on)
 #pragma unroll
             for (int c = 0; c < HELD; ++c) {
-                const int r = c / per, k = at_k(c), piece = k >> 4;
+                const int r = c >> lg, k = at_k(c), piece = k >> 4;
                 if (r >= M) break;
-                const GroupScale& gr = r == 0 ? g[0] : r == 1 ? g[1] : r == 2 ? g[2] : g[3];
+                GroupScale gr = g[0];
+#pragma unroll
+                for (int q = 1; q < SKINNY_FEW; ++q) {
+                    gr.factor = r == q ? g[q].factor : gr.factor;
+                    gr.lift = r == q ? g[q].lift : gr.lift;
+                    gr.finite = r == q ? g[q].finite : gr.finite;
+                }
                 // (zeros behind the row's end, as far as its last k tile goes)
                 if (k < nkt * 128)
                     *reinterpret_cast<i32x2*>(few + r * (nkt * 128) + (piece >> 3) * 128 + ((piece & 7) ^ r) * 16 + (k & 8)) = quantize_chunk<OUT>(v[c], gr);
