@@ -531,8 +531,8 @@ int abft_kv_read(const abft_kv_cache_t *cache /* host */, int tokens, const int6
  *          no initialisation.  Calls that share one must be ordered on one stream.
  * The products run on the matrix unit in the type of Q (int8 keys and values are exact there), softmax statistics
  * and sums in fp32; the weights w_j are rounded to the type of Q.  The scheme of this library's products does not extend to these
- * two: they are not checked.  Results do not depend on the other sequences of the call, but for the split of long key ranges,
- * which follows n_seqs, total_q, max_q and max_kv. */
+ * two: they are not checked.  The same call gives the same bits.  A sequence's results do not depend on the other sequences but in
+ * where long key ranges are cut, and their sums taken apart: that follows the lengths of all of them. */
 int abft_attention(const abft_kv_cache_t *cache /* host */, int n_seqs, const int32_t *q_start, const int32_t *kv_len,
                    const int32_t *block_table, int64_t ld_table, int total_q, int max_q, int max_kv, const void *Q,
                    int64_t ldq, int q_heads, int dtype, float scale, int causal, int window, void *O, int64_t ldo,

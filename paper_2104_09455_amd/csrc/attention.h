@@ -40,10 +40,10 @@ struct AttnArgs {
     // Sequences of one new token have a kernel of their own (single: they are left to it): `single_groups` workgroups, and two
     // places each for sums of keys that are not all of a row's: group rows of dim floats, and of two (m, the sum of weights).
     int single, single_groups;
-    unsigned* counters;                 // one for each of them, zero before and after a launch
+    unsigned* counters;                 // one for each of them or of the row tiles below, zero before and after a launch
     float *single_o, *single_ml;
-    // The others; tile_split: their keys may be divided, and the pieces' sums go here, row tiles of the same.
-    int tile_split;
+    // The others: at most `tiles` row tiles; tile_split: their keys may be divided, and the pieces' sums go here, row tiles of the same.
+    int tiles, tile_split;
     float *tile_o, *tile_ml;
 };
 
@@ -111,6 +111,16 @@ __device__ __forceinline__ void value_scale(float t, float& log2_t, float& inv_t
     t = t < 7.8886091e-31f ? 7.8886091e-31f : t;
     log2_t = __builtin_amdgcn_logf(t);
     inv_t = __builtin_amdgcn_rcpf(t);
+}
+
+// two floats that workgroups on other dies read in the same launch, and read so
+__device__ __forceinline__ void put_shared(float* p, float a, float b) {
+    const unsigned long long v = (unsigned long long)bitcast<unsigned>(b) << 32 | bitcast<unsigned>(a);
+    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_shared(const float* p) {
+    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return float2{bitcast<float>((unsigned)v), bitcast<float>((unsigned)(v >> 32))};
 }
 
 constexpr float ATTN_NONE = -3.402823466e+38f;   // the running maximum before the first key

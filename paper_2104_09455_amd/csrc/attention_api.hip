@@ -22,6 +22,7 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr int MAX_KV = 1 << 24;
 constexpr int COMPUTE_UNITS = 256, COUNTERS = COMPUTE_UNITS * 4;
+static_assert(2 * TILE_SLOTS <= COUNTERS, "one for each row tile of a head that may be in pieces");
 
 // How a call's work is divided, from what the host knows of it.
 struct Division {
@@ -59,8 +60,9 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
     take(COUNTERS);
     d.off_single_o = take(places * c->head_dim);
     d.off_single_ml = take(places * 2);
-    d.off_tile_o = take(rows * c->head_dim);
-    d.off_tile_ml = take(rows * 2);
+    // (a row's sums as they lie in two lanes' registers)
+    d.off_tile_o = take(rows * align_up(c->head_dim, 32));
+    d.off_tile_ml = take(rows * 4);
     d.bytes = at;
     return d;
 }
@@ -111,7 +113,7 @@ int abft_attention(const abft_kv_cache_t* cache, int n_seqs, const int32_t* q_st
     a.c = scale * 1.44269504f;
     a.causal = causal != 0; a.window = window;
     a.single = d.single;
-    a.single_groups = d.single_groups; a.tile_split = d.tile_split;
+    a.single_groups = d.single_groups; a.tiles = d.tiles; a.tile_split = d.tile_split;
     a.counters = reinterpret_cast<unsigned*>(ws);
     a.single_o = reinterpret_cast<float*>(ws + d.off_single_o); a.single_ml = reinterpret_cast<float*>(ws + d.off_single_ml);
     a.tile_o = reinterpret_cast<float*>(ws + d.off_tile_o); a.tile_ml = reinterpret_cast<float*>(ws + d.off_tile_ml);

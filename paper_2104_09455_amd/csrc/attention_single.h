@@ -84,15 +84,6 @@ struct Joint {
     unsigned owner0, owners, place0;
     int token, head;
 };
-// two floats that workgroups on other dies read in the same launch, and read so
-__device__ __forceinline__ void put_shared(float* p, float a, float b) {
-    const unsigned long long v = (unsigned long long)bitcast<unsigned>(b) << 32 | bitcast<unsigned>(a);
-    __hip_atomic_store(reinterpret_cast<unsigned long long*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get_shared(const float* p) {
-    const unsigned long long v = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return float2{bitcast<float>((unsigned)v), bitcast<float>((unsigned)(v >> 32))};
-}
 // VD values of a row from d0 on, divided by the sum of weights
 template <int DT, int VD>
 __device__ __forceinline__ void single_store(const AttnArgs& p, int token, int qh, int d0, const float (&acc)[VD], float norm) {

@@ -27,7 +27,7 @@ constexpr int TILE_SLOTS = 512, TILE_MIN_CHUNK = 8;
 // (pieces of one head beyond one for each row tile: the sum of keys / chunk over the tiles is at most twice the work in slots)
 constexpr int tile_more_pieces(int heads) { return (2 * TILE_SLOTS + heads - 1) / heads; }
 struct TileWork {
-    int seq, tile, tiles, piece, pieces, chunk, slot;   // slot: index of the piece among all sequences'
+    int seq, tile, tiles, piece, pieces, chunk, slot, index;   // slot, index: of the piece and of the row tile among all sequences'
 };
 __device__ __forceinline__ int tile_rows(const AttnArgs& p, const SeqInfo& i, int rows) { return p.single && i.nq == 1 ? 0 : (i.nq * p.group + rows - 1) / rows; }
 // tiles of keys that a row tile of the sequence sees, at most
@@ -36,8 +36,7 @@ __device__ __forceinline__ int tile_keys(const AttnArgs& p, const SeqInfo& i, in
     const int seen = p.window > 0 && p.causal ? (min(p.window, i.kv) + rows / p.group + 1) / ATTN_BLOCK_KEYS + 2 : all;
     return max(min(all, seen), 1);
 }
-// The t-th piece (PIECES) or row tile of the launch; false: there is none.  All of a wavefront.
-template <bool PIECES>
+// The t-th piece of the launch; false: there is none.  All of a wavefront.
 __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, TileWork& w) {
     const int lane = threadIdx.x & 63;
     int n = 0, keys = 1, mean = 1, chunk = 1 << 30;
@@ -50,25 +49,31 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, Ti
     };
     if (p.tile_split) {
         unsigned long long work = 0;
+        int tiles = 0;
         for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
             look(s0);
             work += (unsigned long long)n * mean;
+            tiles += n;
         }
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) work += __shfl_xor(work, d);
-        chunk = (int)max((work * p.heads + TILE_SLOTS - 1) / TILE_SLOTS, (unsigned long long)TILE_MIN_CHUNK);
+        for (int d = 1; d < 64; d <<= 1) {
+            work += __shfl_xor(work, d);
+            tiles += __shfl_xor(tiles, d);
+        }
+        // (more than the host counted, where q_start is not what it has to be: no pieces, since there is no room for theirs)
+        if (tiles <= p.tiles) chunk = (int)max((work * p.heads + TILE_SLOTS - 1) / TILE_SLOTS, (unsigned long long)TILE_MIN_CHUNK);
     }
-    int before = 0, slots = 0;
+    int before = 0, tiles_before = 0;
     for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
         if (!p.tile_split || p.n_seqs > 64) look(s0);   // (else it has been)
-        const int pieces = (keys + chunk - 1) / chunk, units = PIECES ? n * pieces : n;
-        int sum = units, slot_sum = n * pieces;   // of this lane's and all lower ones
+        const int pieces = (keys + chunk - 1) / chunk, units = n * pieces;
+        int sum = units, tile_sum = n;   // of this lane's and all lower ones
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(sum, d), slot_up = __shfl_up(slot_sum, d);
+            const int up = __shfl_up(sum, d), tile_up = __shfl_up(tile_sum, d);
             if (lane >= d) {
                 sum += up;
-                slot_sum += slot_up;
+                tile_sum += tile_up;
             }
         }
         const unsigned long long at = __ballot(before + sum > t);
@@ -78,13 +83,14 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, Ti
             w.tiles = readlane(n, first);
             w.pieces = readlane(pieces, first);
             w.chunk = __builtin_amdgcn_readfirstlane(chunk);
-            w.tile = PIECES ? in / w.pieces : in;
-            w.piece = PIECES ? in - w.tile * w.pieces : 0;
-            w.slot = slots + readlane(slot_sum, first) - w.tiles * w.pieces + w.tile * w.pieces + w.piece;
+            w.tile = in / w.pieces;
+            w.piece = in - w.tile * w.pieces;
+            w.slot = t;
+            w.index = tiles_before + readlane(tile_sum, first) - w.tiles + w.tile;
             return true;
         }
         before += readlane(sum, 63);
-        slots += readlane(slot_sum, 63);
+        tiles_before += readlane(tile_sum, 63);
     }
     return false;
 }
@@ -129,7 +135,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
 
     const int head = (int)blockIdx.x % p.heads;
     TileWork work;
-    if (!find_tile<true>(p, (int)blockIdx.x / p.heads, T::ROWS, work)) return;
+    if (!find_tile(p, (int)blockIdx.x / p.heads, T::ROWS, work)) return;
     const int seq = work.seq, tile = work.tiles - 1 - work.tile;   // (the rows that see most first)
     // (what is the workgroup's or the wavefront's goes into scalar registers, or branches and addresses end up in vector code)
     auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
@@ -153,7 +159,10 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     const int w_full_from = scalar(lo_of(wrow_end)), w_full_to = scalar(hi_of(wrow0));
     // tiles of keys: the row tile's, and the piece's
     const int all0 = from / KEYS, all1 = to > from ? (to + KEYS - 1) / KEYS : all0;
-    const int t0 = scalar(work.piece == 0 ? all0 : min(all0 + work.piece * work.chunk, all1)), t1 = scalar(work.piece == work.pieces - 1 ? all1 : min(t0 + work.chunk, all1));
+    // (a sequence's pieces are enough for the row tile that sees most; others may have fewer)
+    const int pieces = scalar(min(work.pieces, max((all1 - all0 + work.chunk - 1) / work.chunk, 1))), piece = scalar(work.piece);
+    if (piece >= pieces) return;
+    const int t0 = scalar(all0 + piece * work.chunk), t1 = scalar(piece == pieces - 1 ? all1 : t0 + work.chunk);
     // ---- this lane's query, as the fragments of the first product want it: values 16 s + 8 h .. + 7 of its row
     const int token = si.q0 + my_row / p.group, qh = head * p.group + my_row % p.group;
     i32x4 q[STEPS];
@@ -525,90 +534,75 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
         }
     }
 
-    // ---- out: this lane's row, values 32 b + 8 (r / 4) + 4 h + r % 4
     l += swap_halves(l);
+    if (pieces > 1) {
+        // ---- whoever is the last of a row tile's pieces puts their sums together, in the order of the pieces.  (They are written through
+        // to where every die reads them, as they lie in the registers, and waited for, before the counter moves.  A second kernel
+        // for it took 8 to 10 us, and 6 where no row tile was in pieces.)
+        constexpr int PAIRS = 8 * BLOCKS;
+        const long long first = (long long)(work.slot - piece) * p.heads + head;
+        auto place_of = [&](int i) { return ((first + (long long)i * p.heads) * 4 + wave) * 64 + lane; };   // (in twos of floats; of sums, PAIRS times that)
+        auto sums_of = [&](int i) { return p.tile_o + ((place_of(i) - lane) * PAIRS + lane) * 2; };
+        {
+            float* const mine = sums_of(piece);
+#pragma unroll
+            for (int k = 0; k < PAIRS; ++k) put_shared(mine + k * 128, o[k / 8][2 * (k % 8)], o[k / 8][2 * (k % 8) + 1]);
+            put_shared(p.tile_ml + place_of(piece) * 2, m, l);
+        }
+        unsigned* const counter = p.counters + work.index * p.heads + head;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (tid == 0) *special = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)pieces - 1;
+        __syncthreads();
+        if (*special == 0) return;
+        if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // (zero again when the launch ends)
+        float2 ml0, ml1, x0[PAIRS], x1[PAIRS];   // two pieces on their way
+        auto fetch = [&](int i, float2& ml, float2 (&x)[PAIRS]) {
+            const float* const from = sums_of(i);
+            ml = get_shared(p.tile_ml + place_of(i) * 2);
+#pragma unroll
+            for (int k = 0; k < PAIRS; ++k) x[k] = get_shared(from + k * 128);
+        };
+        auto add = [&](const float2& ml, const float2 (&x)[PAIRS]) {
+            const float top = __builtin_fmaxf(m, ml.x), f0 = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+            m = top;
+            l = __builtin_fmaf(f, ml.y, l * f0);
+#pragma unroll
+            for (int k = 0; k < PAIRS; ++k) {
+                o[k / 8][2 * (k % 8)] = __builtin_fmaf(f, x[k].x, o[k / 8][2 * (k % 8)] * f0);
+                o[k / 8][2 * (k % 8) + 1] = __builtin_fmaf(f, x[k].y, o[k / 8][2 * (k % 8) + 1] * f0);
+            }
+        };
+        m = ATTN_NONE;
+        l = 0.f;
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
+        fetch(0, ml0, x0);
+        for (int i = 0; i < pieces; i += 2) {
+            fetch(min(i + 1, pieces - 1), ml1, x1);
+            add(ml0, x0);
+            if (i + 1 < pieces) {
+                fetch(min(i + 2, pieces - 1), ml0, x0);
+                add(ml1, x1);
+            }
+        }
+    }
+    // ---- out: this lane's row, values 32 b + 8 (r / 4) + 4 h + r % 4
     if (!row_on) return;
-    if (work.pieces == 1) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        char* const dst = p.O + (token * p.ldo + (long long)qh * p.dim) * 2;
-#pragma unroll
-        for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int d = 32 * b + 2 * r + 4 * h;
-                i32x2 v;
-                v[0] = pack_out16<DT>(o[b][r] * inv, o[b][r + 1] * inv);
-                v[1] = pack_out16<DT>(o[b][r + 2] * inv, o[b][r + 3] * inv);
-                if (d < p.dim) *reinterpret_cast<i32x2*>(dst + 2 * d) = v;
-            }
-    } else {
-        const long long place = ((long long)work.slot * p.heads + head) * T::ROWS + wave * 32 + col;
-        float* const dst = p.tile_o + place * p.dim;
-        if (h == 0) *reinterpret_cast<float2*>(p.tile_ml + 2 * place) = float2{m, l};
-        if (t1 == t0) return;   // (no weights: the sums are not read)
-#pragma unroll
-        for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; r += 4) {
-                const int d = 32 * b + 2 * r + 4 * h;
-                if (d < p.dim) *reinterpret_cast<f32x4*>(dst + d) = f32x4{o[b][r], o[b][r + 1], o[b][r + 2], o[b][r + 3]};
-            }
-    }
-}
-
-// The pieces of rows put together: eight lanes a row, four workgroups a row tile and head.
-template <int DT>
-__global__ __launch_bounds__(256) void attn_tile_join_kernel(const AttnArgs p) {
-    constexpr int ROWS = AttnTile<128>::ROWS;
-    const int head = (int)blockIdx.x % p.heads, quarter = (int)blockIdx.x / p.heads % 4;
-    TileWork work;
-    if (!find_tile<false>(p, (int)blockIdx.x / p.heads / 4, ROWS, work)) return;
-    if (work.pieces == 1) return;
-    const SeqInfo si = seq_info(p, work.seq);
-    const int in_tile = quarter * 32 + (int)threadIdx.x / 8, row = (work.tiles - 1 - work.tile) * ROWS + in_tile;
-    if (row >= si.nq * p.group) return;
-    // sixteen values a lane, four in a row out of every 32
-    const int part = (threadIdx.x & 7) * 4;
-    float M = ATTN_NONE, L = 0.f;
-    f32x4 acc[4];
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const long long place = ((long long)work.slot * p.heads + head) * ROWS + in_tile, step = (long long)p.heads * ROWS;
-    for (int i0 = 0; i0 < work.pieces; i0 += 4) {
-        // four pieces on their way at a time
-        float2 ml[4];
-        f32x4 x[4][4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const long long at = place + min(i0 + u, work.pieces - 1) * step;
-            ml[u] = *reinterpret_cast<const float2*>(p.tile_ml + 2 * at);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) x[u][c] = *reinterpret_cast<const f32x4*>(p.tile_o + at * p.dim + (32 * c + part < p.dim ? 32 * c + part : 0));
-        }
-        const float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(ml[0].x, ml[1].x), __builtin_fmaxf(ml[2].x, ml[3].x)), M);
-        const float f0 = __builtin_amdgcn_exp2f(M - top);
-        M = top;
-        L *= f0;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) acc[c] *= f0;
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (i0 + u >= work.pieces || ml[u].y == 0.f) continue;
-            const float f = __builtin_amdgcn_exp2f(ml[u].x - M);
-            L = __builtin_fmaf(f, ml[u].y, L);
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[c][e] = __builtin_fmaf(f, x[u][c][e], acc[c][e]);
-        }
-    }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    const int token = si.q0 + row / p.group, qh = head * p.group + row % p.group;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
     char* const dst = p.O + (token * p.ldo + (long long)qh * p.dim) * 2;
 #pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (32 * c + part < p.dim)
-            *reinterpret_cast<i32x2*>(dst + 2 * (32 * c + part)) = i32x2{pack_out16<DT>(acc[c][0] * inv, acc[c][1] * inv), pack_out16<DT>(acc[c][2] * inv, acc[c][3] * inv)};
+    for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+            const int d = 32 * b + 2 * r + 4 * h;
+            i32x2 v;
+            v[0] = pack_out16<DT>(o[b][r] * inv, o[b][r + 1] * inv);
+            v[1] = pack_out16<DT>(o[b][r + 2] * inv, o[b][r + 3] * inv);
+            if (d < p.dim) *reinterpret_cast<i32x2*>(dst + 2 * d) = v;
+        }
 }
 
 }  // namespace abft
