@@ -37,7 +37,7 @@ struct AttnArgs {
     int group;                          // query heads for each head of the cache
     float c;                            // scale log2(e)
     int causal, window;
-    // Sequences of one new token have a kernel of their own (single: they are left to it): `single_groups` workgroups, and two
+    // Sequences of one new token have a program of their own (single: they are left to it): `single_groups` workgroups, and two
     // places each for sums of keys that are not all of a row's: group rows of dim floats, and of two (m, the sum of weights).
     int single, single_groups;
     unsigned* counters;                 // one for each of them or of the row tiles below, zero before and after a launch

@@ -9,8 +9,8 @@
 #include "attention_tile.h"
 
 namespace abft {
-hipError_t launch_attention_f16(const AttnArgs& a, bool i8, int tiles, hipStream_t stream);
-hipError_t launch_attention_bf16(const AttnArgs& a, bool i8, int tiles, hipStream_t stream);
+hipError_t launch_attention_f16(const AttnArgs& a, bool i8, hipStream_t stream);
+hipError_t launch_attention_bf16(const AttnArgs& a, bool i8, hipStream_t stream);
 }  // namespace abft
 
 using namespace abft;
@@ -22,7 +22,10 @@ size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 constexpr int MAX_KV = 1 << 24;
 constexpr int COMPUTE_UNITS = 256, COUNTERS = COMPUTE_UNITS * 4;
-static_assert(2 * TILE_SLOTS <= COUNTERS, "one for each row tile of a head that may be in pieces");
+// Workgroups of single tokens in a launch that has chunks too: beside each of them a compute unit has room for one of a chunk, which
+// multiplies while this one waits for memory.  (Batch of 3 chunks and 5 single tokens over 8000, 28 heads, fp16 cache: 100 us in two
+// launches, 75 in one; 48 single tokens and 512 new ones, 32 heads, int8: 123 / 117, and 127 with twice as many.)
+constexpr int MIXED_GROUPS = COMPUTE_UNITS;
 
 // How a call's work is divided, from what the host knows of it.
 struct Division {
@@ -40,13 +43,13 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
     if (d.single) {
         // all workgroups that the chip holds, if the keys give four units for each
         const long long units = cdiv(max_kv, SINGLE_UNIT) * n * c->heads;
-        const int most = COMPUTE_UNITS * single_per_cu(c->head_dim <= 64 ? 64 : 128);
+        const int most = tiled ? MIXED_GROUPS : COMPUTE_UNITS * single_per_cu(c->head_dim <= 64 ? 64 : 128);
         d.single_groups = (int)std::min<long long>(most, std::max<long long>(std::min<long long>((long long)n * c->heads, most), cdiv(units, 4)));
     }
     if (tiled) {
         d.tiles = n + (int)((long long)total_q * group / AttnTile<128>::ROWS);
-        // (with two tiles for each workgroup that the chip holds, the rows alone fill it)
-        d.tile_split = (long long)d.tiles * c->heads < 2 * TILE_SLOTS && max_kv > TILE_MIN_CHUNK * ATTN_BLOCK_KEYS;
+        // (as long as there is a counter for each row tile: with two of them for each workgroup that the chip holds, the rows fill it)
+        d.tile_split = d.single_groups + (long long)d.tiles * c->heads <= COUNTERS && max_kv > TILE_MIN_CHUNK * ATTN_BLOCK_KEYS;
     }
     size_t at = 0;
     auto take = [&](size_t floats) {
@@ -117,8 +120,7 @@ int abft_attention(const abft_kv_cache_t* cache, int n_seqs, const int32_t* q_st
     a.counters = reinterpret_cast<unsigned*>(ws);
     a.single_o = reinterpret_cast<float*>(ws + d.off_single_o); a.single_ml = reinterpret_cast<float*>(ws + d.off_single_ml);
     a.tile_o = reinterpret_cast<float*>(ws + d.off_tile_o); a.tile_ml = reinterpret_cast<float*>(ws + d.off_tile_ml);
-    const hipError_t e = (dtype == ABFT_F16 ? launch_attention_f16 : launch_attention_bf16)(a, cache->dtype == ABFT_I8, d.tiles,
-                                                                                           reinterpret_cast<hipStream_t>(stream));
+    const hipError_t e = (dtype == ABFT_F16 ? launch_attention_f16 : launch_attention_bf16)(a, cache->dtype == ABFT_I8, reinterpret_cast<hipStream_t>(stream));
     return e == hipSuccess ? ABFT_OK : ABFT_E_HIP;
 }
 

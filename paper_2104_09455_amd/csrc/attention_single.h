@@ -93,17 +93,23 @@ __device__ __forceinline__ void single_store(const AttnArgs& p, int token, int q
         *reinterpret_cast<i32x2*>(dst + 2 * j) = i32x2{pack_out16<DT>(acc[j] * norm, acc[j + 1] * norm), pack_out16<DT>(acc[j + 2] * norm, acc[j + 3] * norm)};
 }
 
+template <int DP>
+struct __attribute__((aligned(16))) SingleLds {
+    float o[4][16][DP];   // the wavefronts' sums
+    float m[4][16], l[4][16];
+    bool last_owner[2];
+};
 template <int DT, bool I8, int DP>
-__global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(const AttnArgs p) {
+__device__ __forceinline__ void single_tokens(const AttnArgs& p, SingleLds<DP>& lds) {
     typedef Mma<DT, 16> MMA;
     constexpr int ES = I8 ? 1 : 2, STEPS = DP / 32;
     constexpr int KB = DP / 4 * ES / 16;    // 16-byte pieces of a key in a lane: a quarter of its values
     constexpr int VD = DP / 16;             // values of a V row in a lane
     constexpr int VW = VD * ES / 4;         // registers of them
     typedef int Piece __attribute__((ext_vector_type(VW)));
-    __shared__ __attribute__((aligned(16))) float out_o[4][16][DP];
-    __shared__ float out_m[4][16], out_l[4][16];
-    __shared__ bool last_owner[2];
+    auto& out_o = lds.o;
+    auto &out_m = lds.m, &out_l = lds.l;
+    auto& last_owner = lds.last_owner;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 15, g = lane >> 4;
@@ -444,6 +450,12 @@ __global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(con
         }
         __syncthreads();
     }
+}
+
+template <int DT, bool I8, int DP>
+__global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(const AttnArgs p) {
+    __shared__ SingleLds<DP> lds;
+    single_tokens<DT, I8, DP>(p, lds);
 }
 
 }  // namespace abft

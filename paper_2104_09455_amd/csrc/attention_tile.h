@@ -2,6 +2,7 @@
 // tokens' query heads of that head, token by token), and all keys that these rows see, 64 at a time, in 16 bits in LDS.
 #pragma once
 #include "attention.h"
+#include "attention_single.h"
 
 namespace abft {
 
@@ -123,19 +124,30 @@ __device__ __forceinline__ void add_not_finite(const AttnArgs& p, f32x16 (&o)[DP
 }
 
 // PAD: heads of fewer than DP values (16-bit caches; int8 ones do not care)
-template <int DT, bool I8, int DP, bool PAD>
+// MIXED: the batch has single tokens too, which the launch's first workgroups take
+template <int DT, bool I8, int DP, bool PAD, bool MIXED>
 __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     typedef AttnTile<DP> T;
     typedef Mma<DT, 32> MMA;
     constexpr int STEPS = DP / 16, BLOCKS = DP / 32, KEYS = T::KEYS;
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    unsigned bid = blockIdx.x;
+    if constexpr (MIXED) {
+        constexpr int SINGLE_DP = DP <= 64 ? 64 : 128;
+        static_assert(sizeof(SingleLds<SINGLE_DP>) <= T::LDS_BYTES, "in the same place");
+        if (bid < (unsigned)p.single_groups) {
+            single_tokens<DT, I8, SINGLE_DP>(p, *reinterpret_cast<SingleLds<SINGLE_DP>*>(smem));
+            return;
+        }
+        bid -= p.single_groups;
+    }
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int col = lane & 31, h = lane >> 5;   // this lane's row of the wavefront's 32, its half of the keys
 
-    const int head = (int)blockIdx.x % p.heads;
+    const int head = (int)(bid % (unsigned)p.heads);
     TileWork work;
-    if (!find_tile(p, (int)blockIdx.x / p.heads, T::ROWS, work)) return;
+    if (!find_tile(p, (int)(bid / (unsigned)p.heads), T::ROWS, work)) return;
     const int seq = work.seq, tile = work.tiles - 1 - work.tile;   // (the rows that see most first)
     // (what is the workgroup's or the wavefront's goes into scalar registers, or branches and addresses end up in vector code)
     auto scalar = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
@@ -549,7 +561,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
             for (int k = 0; k < PAIRS; ++k) put_shared(mine + k * 128, o[k / 8][2 * (k % 8)], o[k / 8][2 * (k % 8) + 1]);
             put_shared(p.tile_ml + place_of(piece) * 2, m, l);
         }
-        unsigned* const counter = p.counters + work.index * p.heads + head;
+        unsigned* const counter = p.counters + (MIXED ? p.single_groups : 0) + work.index * p.heads + head;
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
         if (tid == 0) *special = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)pieces - 1;
