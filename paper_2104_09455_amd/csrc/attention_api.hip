@@ -41,10 +41,13 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
     d.single = group <= ATTN_GROUP_MAX && (max_q == 1 || (long long)n * max_q != total_q);
     const bool tiled = !d.single || max_q > 1;
     if (d.single) {
-        // all workgroups that the chip holds, if the keys give four units for each
-        const long long units = cdiv(max_kv, SINGLE_UNIT) * n * c->heads;
-        const int most = tiled ? MIXED_GROUPS : COMPUTE_UNITS * single_per_cu(c->head_dim <= 64 ? 64 : 128);
-        d.single_groups = (int)std::min<long long>(most, std::max<long long>(std::min<long long>((long long)n * c->heads, most), cdiv(units, 4)));
+        // Workgroups: one a unit up to 128, and more, up to one a compute unit, for four units each; two a compute unit with 256 heads of
+        // sequences, and as many as there are heads in any case, so that fewer of them are shared.  (One token of 2048, int8, 128
+        // wide: 64 / 128 workgroups 11.3 / 10.7 us; of 4096 128 / 256 11.7 / 12.5; of 32768 256 / 512 21.1 / 26.4; 16 of 8192 57.6 / 59.7; 64
+        // of 4096 120.6 / 105.2 and with three a compute unit 117, where shares end inside more heads; 64 of 300 16.7 / 13.0 / 20.3.)
+        const long long heads = (long long)n * c->heads, units = cdiv(max_kv, SINGLE_UNIT) * heads;
+        const long long most = tiled ? MIXED_GROUPS : heads < COMPUTE_UNITS ? COMPUTE_UNITS : 2 * COMPUTE_UNITS;
+        d.single_groups = (int)std::min(most, std::max({heads, std::min(units, 128ll), cdiv(units, 4)}));
     }
     if (tiled) {
         d.tiles = n + (int)((long long)total_q * group / AttnTile<128>::ROWS);

@@ -1,16 +1,17 @@
 // One new token: its rows are the up to sixteen query heads of a head of the cache.  The keys of all such sequences and heads,
-// put behind one another in units of 128, are divided evenly over as many workgroups as the chip holds at once, so that all
+// put behind one another in units of 128, are divided evenly over one or two workgroups for each compute unit, so that all
 // end together whatever the lengths are; a workgroup's share begins and ends anywhere, and may span several heads and
 // sequences.  Its four wavefronts take 32 keys each in turn, straight from memory into fragments (nothing is read twice,
 // so nothing goes through LDS); at the end of a head's keys, or of the share, their sums meet in LDS.
-// Bound: the bytes of keys and values.
+// Bound: the bytes of keys and values, and for few sequences the chain of loads, stores and counters behind one another.  Measured, 8 heads of
+// 128 read by 4 queries each: 64 sequences of 17 to 8144 tokens, int8, 110 us (5.0 TB/s); 16 of 8192, fp16, 100 us (5.4 TB/s), int8 57 (4.8);
+// one of 2048 / 32768, int8, 10.6 / 20.8 us.
 #pragma once
 #include "attention.h"
 
 namespace abft {
 
 constexpr int SINGLE_UNIT = 128;
-constexpr int single_per_cu(int dp) { return dp == 64 ? 4 : 3; }   // workgroups that a compute unit holds (registers)
 
 // the first key that a single token sees (it is the last one itself), and its units: one at least, since its rows have to be written
 __device__ __forceinline__ int single_lo(const AttnArgs& p, int kv) { return p.window > 0 ? max(kv - p.window, 0) : 0; }
@@ -453,7 +454,7 @@ __device__ __forceinline__ void single_tokens(const AttnArgs& p, SingleLds<DP>& 
 }
 
 template <int DT, bool I8, int DP>
-__global__ __launch_bounds__(256, single_per_cu(DP)) void attn_single_kernel(const AttnArgs p) {
+__global__ __launch_bounds__(256, 2) void attn_single_kernel(const AttnArgs p) {
     __shared__ SingleLds<DP> lds;
     single_tokens<DT, I8, DP>(p, lds);
 }

@@ -100,7 +100,8 @@ struct QuantizeArgs {
 
 // Rows of a matrix.  TPR threads share a row and hold it in registers between the two passes (NV chunks of eight values each);
 // with NV = 0 they read it twice.
-// Bound: the row's bytes once, 2 K in and K out; few rows: one round trip to them.
+// Bound: the row's bytes once, 2 K in and K out; few rows: one round trip to them.  Measured: 8192 x 8192 29.7 us (6.8 TB/s), 64 x
+// 8192 3.0 us.
 template <int DT, int TPR, int NV>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs p) {
     __shared__ unsigned tops[4];
@@ -154,7 +155,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs p
 
 template <int DT>
 inline hipError_t launch_quantize_rows(const QuantizeArgs& a, hipStream_t stream) {
-    // (a wavefront per row where four chunks a lane hold it and there are rows enough to fill the chip so; else a workgroup)
+    // (a wavefront per row where four chunks a lane hold it and there are rows enough to fill the chip so; else a workgroup.  us,
+    // wavefront / workgroup: 8192 x 512 3.6 / 5.8, 64 x 512 2.35 / 2.42; 8192 x 2048 8.6 / 9.8, 4096 x 1024 3.6 / 4.3, 1024 x 2048 level, 256 x 2048
+    // 2.9 / 2.5.  Rows that do not fit the registers are read twice.)
     void (*kern)(const QuantizeArgs);
     int rows = 1;
     if (a.K <= 512) { kern = quantize_rows_kernel<DT, 64, 1>; rows = 4; }
