@@ -119,7 +119,7 @@ int abft_attention(const abft_kv_cache_t* cache, int n_seqs, const int32_t* q_st
     a.c = scale * 1.44269504f;
     a.causal = causal != 0; a.window = window;
     a.single = d.single;
-    a.single_groups = d.single_groups; a.tiles = d.tiles; a.tile_split = d.tile_split;
+    a.single_groups = d.single_groups; a.tiles = d.tiles; a.tile_split = d.tile_split; a.tile_counters = COUNTERS - d.single_groups;
     a.counters = reinterpret_cast<unsigned*>(ws);
     a.single_o = reinterpret_cast<float*>(ws + d.off_single_o); a.single_ml = reinterpret_cast<float*>(ws + d.off_single_ml);
     a.tile_o = reinterpret_cast<float*>(ws + d.off_tile_o); a.tile_ml = reinterpret_cast<float*>(ws + d.off_tile_ml);

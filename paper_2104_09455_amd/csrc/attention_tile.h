@@ -29,7 +29,12 @@ constexpr int TILE_SLOTS = 512, TILE_MIN_CHUNK = 8;
 constexpr int tile_more_pieces(int heads) { return (2 * TILE_SLOTS + heads - 1) / heads; }
 struct TileWork {
     int seq, tile, tiles, piece, pieces, chunk, slot, index;   // slot, index: of the piece and of the row tile among all sequences'
+    int group;   // the counter of the row tile's first group of pieces, -1: they are joined all at once
 };
+// A workgroup that joins many pieces' sums (64 KB each) takes long over them: from TILE_MANY on they are joined in groups first, and
+// then the groups.  (16 new tokens of 32768, 8 x 4 heads, 64 pieces: 99 us at once, 49.5 in groups; 128 of 8192, 16 pieces: 65 / 57.5.)
+constexpr int TILE_MANY = 13, TILE_GROUP = 8;
+__device__ __forceinline__ int tile_groups(int pieces) { return pieces < TILE_MANY ? 0 : (pieces + TILE_GROUP - 1) / TILE_GROUP; }
 __device__ __forceinline__ int tile_rows(const AttnArgs& p, const SeqInfo& i, int rows) { return p.single && i.nq == 1 ? 0 : (i.nq * p.group + rows - 1) / rows; }
 // tiles of keys that a row tile of the sequence sees, at most
 __device__ __forceinline__ int tile_keys(const AttnArgs& p, const SeqInfo& i, int rows) {
@@ -40,7 +45,7 @@ __device__ __forceinline__ int tile_keys(const AttnArgs& p, const SeqInfo& i, in
 // The t-th piece of the launch; false: there is none.  All of a wavefront.
 __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, TileWork& w) {
     const int lane = threadIdx.x & 63;
-    int n = 0, keys = 1, mean = 1, chunk = 1 << 30;
+    int n = 0, keys = 1, mean = 1, chunk = 1 << 30, all_tiles = 0;
     auto look = [&](int s0) {
         const SeqInfo i = seq_info(p, min(s0 + lane, p.n_seqs - 1));
         n = s0 + lane < p.n_seqs ? tile_rows(p, i, rows) : 0;
@@ -62,19 +67,21 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, Ti
             tiles += __shfl_xor(tiles, d);
         }
         // (more than the host counted, where q_start is not what it has to be: no pieces, since there is no room for theirs)
+        all_tiles = tiles;
         if (tiles <= p.tiles) chunk = (int)max((work * p.heads + TILE_SLOTS - 1) / TILE_SLOTS, (unsigned long long)TILE_MIN_CHUNK);
     }
-    int before = 0, tiles_before = 0;
+    int before = 0, tiles_before = 0, groups_before = all_tiles;
     for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
         if (!p.tile_split || p.n_seqs > 64) look(s0);   // (else it has been)
-        const int pieces = (keys + chunk - 1) / chunk, units = n * pieces;
-        int sum = units, tile_sum = n;   // of this lane's and all lower ones
+        const int pieces = (keys + chunk - 1) / chunk, units = n * pieces, groups = n * tile_groups(pieces);
+        int sum = units, tile_sum = n, group_sum = groups;   // of this lane's and all lower ones
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(sum, d), tile_up = __shfl_up(tile_sum, d);
+            const int up = __shfl_up(sum, d), tile_up = __shfl_up(tile_sum, d), group_up = __shfl_up(group_sum, d);
             if (lane >= d) {
                 sum += up;
                 tile_sum += tile_up;
+                group_sum += group_up;
             }
         }
         const unsigned long long at = __ballot(before + sum > t);
@@ -88,10 +95,15 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, Ti
             w.piece = in - w.tile * w.pieces;
             w.slot = t;
             w.index = tiles_before + readlane(tile_sum, first) - w.tiles + w.tile;
+            // (as far as the counters reach)
+            const int many = tile_groups(w.pieces);
+            w.group = groups_before + readlane(group_sum, first) - (w.tiles - w.tile) * many;
+            if (many == 0 || (w.group + many) * p.heads > p.tile_counters) w.group = -1;
             return true;
         }
         before += readlane(sum, 63);
         tiles_before += readlane(tile_sum, 63);
+        groups_before += readlane(group_sum, 63);
     }
     return false;
 }
@@ -552,23 +564,9 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
         // to where every die reads them, as they lie in the registers, and waited for, before the counter moves.  A second kernel
         // for it took 8 to 10 us, and 6 where no row tile was in pieces.)
         constexpr int PAIRS = 8 * BLOCKS;
-        const long long first = (long long)(work.slot - piece) * p.heads + head;
-        auto place_of = [&](int i) { return ((first + (long long)i * p.heads) * 4 + wave) * 64 + lane; };   // (in twos of floats; of sums, PAIRS times that)
+        const long long first_place = (long long)(work.slot - piece) * p.heads + head;
+        auto place_of = [&](int i) { return ((first_place + (long long)i * p.heads) * 4 + wave) * 64 + lane; };   // (in twos of floats; of sums, PAIRS times that)
         auto sums_of = [&](int i) { return p.tile_o + ((place_of(i) - lane) * PAIRS + lane) * 2; };
-        {
-            float* const mine = sums_of(piece);
-#pragma unroll
-            for (int k = 0; k < PAIRS; ++k) put_shared(mine + k * 128, o[k / 8][2 * (k % 8)], o[k / 8][2 * (k % 8) + 1]);
-            put_shared(p.tile_ml + place_of(piece) * 2, m, l);
-        }
-        unsigned* const counter = p.counters + (MIXED ? p.single_groups : 0) + work.index * p.heads + head;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (tid == 0) *special = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)pieces - 1;
-        __syncthreads();
-        if (*special == 0) return;
-        if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // (zero again when the launch ends)
-        float2 ml0, ml1, x0[PAIRS], x1[PAIRS];   // two pieces on their way
         auto fetch = [&](int i, float2& ml, float2 (&x)[PAIRS]) {
             const float* const from = sums_of(i);
             ml = get_shared(p.tile_ml + place_of(i) * 2);
@@ -585,20 +583,53 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
                 o[k / 8][2 * (k % 8) + 1] = __builtin_fmaf(f, x[k].y, o[k / 8][2 * (k % 8) + 1] * f0);
             }
         };
-        m = ATTN_NONE;
-        l = 0.f;
+        // who meets here: `count` pieces from `first` on, every step-th; the sums so far are those of piece `mine`
+        unsigned* const counters = p.counters + (MIXED ? p.single_groups : 0);
+        unsigned* counter = counters + work.index * p.heads + head;
+        int mine = piece, first = 0, step = 1, count = pieces;
+        const bool grouped = scalar(work.group) >= 0 && pieces > TILE_GROUP;
+        if (grouped) {
+            first = piece / TILE_GROUP * TILE_GROUP;
+            count = min(TILE_GROUP, pieces - first);
+            counter = counters + (work.group + piece / TILE_GROUP) * p.heads + head;
+        }
+        for (bool last = !grouped;; last = true) {
+            if (wave_on) {
+                float* const to = sums_of(mine);
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
-        fetch(0, ml0, x0);
-        for (int i = 0; i < pieces; i += 2) {
-            fetch(min(i + 1, pieces - 1), ml1, x1);
-            add(ml0, x0);
-            if (i + 1 < pieces) {
-                fetch(min(i + 2, pieces - 1), ml0, x0);
-                add(ml1, x1);
+                for (int k = 0; k < PAIRS; ++k) put_shared(to + k * 128, o[k / 8][2 * (k % 8)], o[k / 8][2 * (k % 8) + 1]);
+                put_shared(p.tile_ml + place_of(mine) * 2, m, l);
             }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tid == 0) *special = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)count - 1;
+            __syncthreads();
+            if (*special == 0) return;
+            if (tid == 0) __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);   // (zero again when the launch ends)
+            if (wave_on) {
+                m = ATTN_NONE;
+                l = 0.f;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
+                float2 ml0, ml1, x0[PAIRS], x1[PAIRS];   // two pieces on their way
+                fetch(first, ml0, x0);
+                for (int i = 0; i < count; i += 2) {
+                    fetch(first + min(i + 1, count - 1) * step, ml1, x1);
+                    add(ml0, x0);
+                    if (i + 1 < count) {
+                        fetch(first + min(i + 2, count - 1) * step, ml0, x0);
+                        add(ml1, x1);
+                    }
+                }
+            }
+            if (last) break;
+            mine = first;
+            first = 0;
+            step = TILE_GROUP;
+            count = (pieces + TILE_GROUP - 1) / TILE_GROUP;
+            counter = counters + work.index * p.heads + head;
         }
     }
     // ---- out: this lane's row, values 32 b + 8 (r / 4) + 4 h + r % 4

@@ -303,3 +303,20 @@ def test_attention_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(want.view(torch.int16), out.view(torch.int16))
+
+
+@pytest.mark.parametrize("dtype,cache", both("bf16") + both("f16"))
+@pytest.mark.parametrize("q,kv,heads,group,dim,window", [
+    ([16], [20000], 2, 4, 128, 0),                          # one row tile of which half is empty, dozens of pieces
+    ([70, 3], [9000, 7777], 1, 8, 64, 0),                   # several row tiles, each with many
+    ([33, 1, 2], [12001, 12001, 40], 2, 3, 80, 0),          # beside single tokens
+    ([16], [30000], 3, 4, 96, 9000),                        # and in a window
+    ([2] * 112, [64] * 111 + [20000], 9, 1, 64, 0),         # more counters wanted than there are
+])
+def test_many_pieces(q, kv, heads, group, dim, window, dtype, cache):
+    c = Case(q, kv, heads, group, dim, 64, dtype, cache, seed=11, window=window)
+    got = c.run()
+    c.check(got)
+    # (whoever comes last joins the pieces: always in the same order)
+    for _ in range(3):
+        assert torch.equal(c.run(), got)
