@@ -1,5 +1,8 @@
 // Many rows: a workgroup of four wavefronts takes 32 rows each of one sequence and head of the cache (rows are the new
 // tokens' query heads of that head, token by token), and all keys that these rows see, 64 at a time, in 16 bits in LDS.
+// Bound: the softmax's vector work beside the MFMAs, and for little work what a piece costs to begin and to join, about 10 us.  Measured, 8 heads of
+// 128 read by 4 queries each: 8192 of 8192 tokens, bf16, 540 us (1010 TFLOP/s); from an int8 cache, which is widened on the way, fp16 690; 2048 of
+// 12000 in a window of 1000, 80 wide, 42.
 #pragma once
 #include "attention.h"
 #include "attention_single.h"
@@ -20,11 +23,13 @@ struct AttnTile {
     static __device__ __forceinline__ int v_swizzle(int r) { return PITCH == 256 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
 };
 
-// The launch's work: row tiles of each sequence, and pieces of the keys that a row tile sees where splitting them pays.  A piece is
-// `chunk` tiles of keys, counted from the row tile's first, the same for all, so many that the whole work makes about one piece
-// for each workgroup that the chip holds, and at least TILE_MIN_CHUNK (a piece's sums cost as much as three or four tiles);
-// the host cannot know, since lengths are on the device.
-constexpr int TILE_SLOTS = 512, TILE_MIN_CHUNK = 8;
+// The launch's work: row tiles of each sequence, and pieces of the keys that a row tile sees where splitting them pays.  A sequence's
+// pieces are of one size, near `chunk` tiles of keys (as many as fit it, one more if more than a quarter would be left over), so large that
+// the whole work makes nine tenths of a piece for each workgroup that the chip holds: a few more than that would be a second round.
+// At least TILE_MIN_CHUNK (a piece's sums cost as much as three or four tiles).  The host cannot know, since lengths are on the device.
+// (us, fp16, 32 heads of 128, against pieces of exactly one for each workgroup, the last of a row tile short, a row tile's pieces beside one another
+// in the launch: 509 of 4605 tokens 65 / 56, 2048 of 2048 78 / 70, 3 x 700 of 5000 316 / 237, 512 of 8192 95 / 90, 1024 of 1024 level.)
+constexpr int TILE_SLOTS = 464, TILE_MIN_CHUNK = 8;
 // (pieces of one head beyond one for each row tile: the sum of keys / chunk over the tiles is at most twice the work in slots)
 constexpr int tile_more_pieces(int heads) { return (2 * TILE_SLOTS + heads - 1) / heads; }
 struct TileWork {
@@ -45,7 +50,7 @@ __device__ __forceinline__ int tile_keys(const AttnArgs& p, const SeqInfo& i, in
 // The t-th piece of the launch; false: there is none.  All of a wavefront.
 __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, TileWork& w) {
     const int lane = threadIdx.x & 63;
-    int n = 0, keys = 1, mean = 1, chunk = 1 << 30, all_tiles = 0;
+    int n = 0, keys = 1, mean = 1, chunk = 1 << 28, all_tiles = 0;
     auto look = [&](int s0) {
         const SeqInfo i = seq_info(p, min(s0 + lane, p.n_seqs - 1));
         n = s0 + lane < p.n_seqs ? tile_rows(p, i, rows) : 0;
@@ -73,7 +78,7 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, Ti
     int before = 0, tiles_before = 0, groups_before = all_tiles;
     for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {
         if (!p.tile_split || p.n_seqs > 64) look(s0);   // (else it has been)
-        const int pieces = (keys + chunk - 1) / chunk, units = n * pieces, groups = n * tile_groups(pieces);
+        const int pieces = max((4 * keys + 3 * chunk) / (4 * chunk), 1), units = n * pieces, groups = n * tile_groups(pieces);
         int sum = units, tile_sum = n, group_sum = groups;   // of this lane's and all lower ones
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
@@ -90,10 +95,11 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, Ti
             w.seq = s0 + first;
             w.tiles = readlane(n, first);
             w.pieces = readlane(pieces, first);
-            w.chunk = __builtin_amdgcn_readfirstlane(chunk);
-            w.tile = in / w.pieces;
-            w.piece = in - w.tile * w.pieces;
-            w.slot = t;
+            w.chunk = readlane((keys + pieces - 1) / pieces, first);
+            // (all first pieces, then all second ones: the long ones begin first and are spread over all compute units)
+            w.piece = in / w.tiles;
+            w.tile = in - w.piece * w.tiles;
+            w.slot = t - in + w.tile * w.pieces + w.piece;
             w.index = tiles_before + readlane(tile_sum, first) - w.tiles + w.tile;
             // (as far as the counters reach)
             const int many = tile_groups(w.pieces);
