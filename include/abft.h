@@ -451,7 +451,8 @@ int abft_quantize_rows(int M, int K, const void *X, int64_t ldx, int dtype, void
  *       exactly, as they do there.
  *   row_scale: M floats (abft_quantize_rows); col_scale: N floats; bias: N floats or NULL.
  *   act: abft_act_t.  C: M x N, ldc >= N, of type out_dtype (F16 / BF16).  C[m][n] is the sum as a float, times row_scale[m], times
- *       col_scale[n] plus bias[n] in one fused step, after the activation function, rounded once to nearest even.
+ *       col_scale[n] plus bias[n] in one fused step, after the activation function, rounded once to nearest even.  NaN in a scale or
+ *       the bias stays through ABFT_ACT_RELU (max(x, 0) of all other values): it comes in behind the checks, which see none of it.
  *   mode: ABFT_NONE, ABFT_GLOBAL, ABFT_THREAD, or ABFT_AUTO (abft_scaled_select); the others: ABFT_E_UNSUPPORTED.
  *   K: at most 131071 (the sums stay within int32), else ABFT_E_SHAPE. */
 int abft_gemm_scaled(int M, int N, int K, const void *A, int64_t lda, const float *row_scale, const void *B, int64_t ldb,

@@ -824,10 +824,11 @@ __device__ __forceinline__ bool cross_wave_last(char* epi, int lane, int wave) {
 __device__ __forceinline__ int relu(int x) { return x > 0 ? x : 0; }
 __device__ __forceinline__ float relu(float x) { return __builtin_amdgcn_fmed3f(x, 3.402823466e+38f, 0.f); }
 
-// One element of a scaled product, ready to be rounded
+// One element of a scaled product, ready to be rounded.  NaN stays through the activation function: it comes in by a scale or the
+// bias, behind the checks, so nothing has raised the flag for it.
 __device__ __forceinline__ float scaled_value(int sum, float row, float col, float bias, int act) {
     const float v = __builtin_fmaf((float)sum * row, col, bias);
-    return act ? relu(v) : v;
+    return act && v < 0.f ? 0.f : v;
 }
 // The scales of up to four consecutive rows; rows outside C take the last one's
 __device__ __forceinline__ f32x4 row_scales(const GemmArgs& p, int row) {

@@ -202,6 +202,39 @@ def test_scales_that_are_nan_or_zero():
     assert torch.isfinite(got[[i for i in range(40) if i != 7]]).all()
 
 
+# (every store of C: the few rows' kernel, skinny, streaming, direct-to-LDS and generic tiles, whole and cut)
+@pytest.mark.parametrize("mode", [B.NONE, B.GLOBAL, B.THREAD])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K,layout", [(1, 96, 64, B.B_NK), (2, 40, 130, B.B_KN), (4, 4096, 256, B.B_NK), (9, 200, 256, B.B_NK), (64, 64, 64, B.B_NK), (100, 33, 1024, B.B_NK),
+                                      (130, 200, 300, B.B_NK), (70, 65, 33, B.B_KN), (512, 520, 512, B.B_NK), (1000, 700, 128, B.B_NK), (1152, 4096, 1024, B.B_NK), (3000, 2100, 257, B.B_NK)])
+def test_relu_keeps_what_is_not_a_number(M, N, K, layout, dtype, mode):
+    """Rows that hold an infinity or a NaN, and columns whose scale or bias is NaN, are NaN behind the activation function too;
+    everything else is what it makes of the layer's values.  (The sums of such a row are zeros: no check sees it.)"""
+    print(f"case relu {M}x{N}x{K} {dtype} mode={mode} layout={layout}", flush=True)
+    p = Product(M, N, K, dtype, layout, seed=M)
+    x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).to(p.t).to(DEV)
+    bad = sorted({0, M // 2, M - 1} - ({0} if 1 < M < 4 else set()))
+    for i, m in enumerate(bad):
+        x[m, (7 * m + 3) % K] = [float("inf"), float("nan"), -float("inf")][(i + M) % 3]
+    p.cs[N // 2], p.bias[N - 1] = float("nan"), float("nan")
+    n = B.abft_linear_scaled_workspace_bytes(M, N, K, mode)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    outs = []
+    for act in (B.ACT_NONE, B.ACT_RELU):
+        outs.append(torch.full((M, N), 7.0, dtype=p.t, device=DEV))
+        B.abft_linear_scaled(M, N, K, x, K, p.dt, p.Bm, p.ldb, layout, p.cs, p.bias, act, outs[-1], N, mode, workspace=ws, workspace_bytes=n, fault_flag=p.flag)
+    torch.cuda.synchronize()
+    plain, got = outs
+    rows = torch.zeros(M, dtype=torch.bool, device=DEV)
+    rows[bad] = True
+    columns = torch.zeros(N, dtype=torch.bool, device=DEV)
+    columns[[N // 2, N - 1]] = True
+    assert torch.equal(torch.isnan(plain), rows[:, None] | columns)
+    assert torch.equal(torch.isnan(got), torch.isnan(plain))
+    number = ~torch.isnan(plain)
+    assert torch.equal(got[number], plain[number].clamp(min=0))
+
+
 @pytest.mark.parametrize("mode", [B.NONE, B.GLOBAL, B.THREAD, B.AUTO])
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("M,N,K,layout", [(1, 96, 64, B.B_NK), (1, 33, 7, B.B_KN), (1, 1, 17, B.B_NK), (2, 40, 130, B.B_NK), (3, 100, 1001, B.B_NK), (4, 4096, 8192, B.B_NK), (4, 50, 8193, B.B_NK), (1, 70, 32768, B.B_NK),
