@@ -222,12 +222,26 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
             __syncthreads();
         }
     };
-    int i = 0;
-    if (n_own > 2 * U) {
-        // (no condition between the loads, so that the number behind the one that is waited for is known)
+    const bool many = n_own > 2 * U;   // (k tiles of this wavefront)
+    auto load_first = [&]() {
+        // (no condition between the loads of many, so that the number behind the one that is waited for is known)
+        if (many) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) load_whole(u, u);
+            for (int u = 0; u < U; ++u) load_whole(u, u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u < n_own) load(u, u);
+        }
+    };
+    int i = 0;
+    // (its barriers are for all wavefronts, also where some have many k tiles and others have not)
+    if constexpr (FEW) {
+        load_first();
         quantise_rows();
+    }
+    if (many) {
+        if constexpr (!FEW) load_first();
 #pragma nounroll
         for (; i + 2 * U < n_own; i += U)
 #pragma unroll
@@ -236,10 +250,7 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
                 load_whole(u, i + U + u);
             }
     } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (u < n_own) load(u, u);
-        quantise_rows();
+        if constexpr (!FEW) load_first();
     }
 #pragma nounroll
     for (; i < n_own; i += U)

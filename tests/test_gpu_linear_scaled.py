@@ -265,6 +265,36 @@ def test_linear_layer_is_its_two_steps(M, N, K, layout, dtype, mode):
     assert torch.equal(out.view(torch.int16), want.contiguous().view(torch.int16))
 
 
+# (one launch: rows of one, two and four chunks a thread; wavefronts with few k tiles, with many, and, at 4225 and 5119, both in a workgroup)
+@pytest.mark.parametrize("mode", [B.NONE, B.THREAD])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(4, 512, 4096), (3, 100, 4095), (2, 512, 8192), (2, 70, 4225), (1, 70, 4225), (1, 512, 16384), (1, 70, 8209), (1, 64, 8320),
+                                   (2, 33, 5119), (1, 33, 16383)])
+def test_few_rows_of_long_products(M, N, K, dtype, mode):
+    """The sums from the quantisation's definition, in 64 bits, and bit for bit the two calls' results."""
+    print(f"case few {M}x{N}x{K} {dtype} mode={mode}", flush=True)
+    p = Product(M, N, K, dtype, B.B_NK, seed=K + M)
+    x = torch.zeros(M, K + 3, dtype=p.t, device=DEV)
+    x[:, :K] = hard_rows(M, K, p.t, seed=K)
+    x[:, K:] = float("nan")
+    n = B.abft_linear_scaled_workspace_bytes(M, N, K, mode)
+    ws = torch.full((n,), 131, dtype=torch.uint8, device=DEV)
+    out = torch.full((M, N), 7.0, dtype=p.t, device=DEV)
+    B.abft_linear_scaled(M, N, K, x, K + 3, p.dt, p.Bm, p.ldb, B.B_NK, p.cs, p.bias, B.ACT_NONE, out, N, mode, workspace=ws, workspace_bytes=n,
+                         fault_flag=p.flag)
+    torch.cuda.synchronize()
+    assert int(p.flag.item()) == 0
+    q, scale = quantised(x[:, :K])
+    p.a, p.rs = q.to(torch.int8).cpu(), scale
+    p.check(out)
+    ldq = -(-K // 16) * 16
+    p.bufs.append(torch.zeros(M, ldq, dtype=torch.int8, device=DEV))
+    p.bufs[-1][:, :K] = q.to(torch.int8)
+    p.A, p.lda = p.bufs[-1].data_ptr(), ldq
+    want, flag = p.run(mode)
+    assert flag == 0 and torch.equal(out.view(torch.int16), want.contiguous().view(torch.int16))
+
+
 @pytest.mark.parametrize("M", [1, 4])
 def test_few_rows_with_a_report_or_a_planted_fault(M):
     """Calls that cannot take the few rows' kernel give its results, and see a fault."""
