@@ -176,7 +176,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     const int rows = si.nq * p.group, before = si.kv - si.nq;
 
     // ---- rows: the workgroup's, the wavefront's, this lane's, and the keys that they see, lo .. hi - 1
-    auto lo_of = [&](int r) { return p.window > 0 ? max(before + r / p.group - p.window + 1, 0) : 0; };
+    // (before may be negative and a window as large as an int is: no difference is taken that could wrap)
+    auto lo_of = [&](int r) { return p.window > 0 ? max(before + r / p.group, p.window - 1) - (p.window - 1) : 0; };
     auto hi_of = [&](int r) { return p.causal ? min(before + r / p.group + 1, si.kv) : si.kv; };
     const int row0 = tile * T::ROWS, row_end = min(row0 + T::ROWS, rows) - 1;
     const int wrow0 = min(row0 + wave * 32, rows - 1), wrow_end = min(row0 + wave * 32 + 31, rows - 1);

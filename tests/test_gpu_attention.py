@@ -171,6 +171,17 @@ def test_chunks(q, kv, heads, group, dim, page, causal, window, dtype, cache):
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES_AND_CACHES)
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 40, 2 ** 30])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("q,kv", [([10, 1, 6], [4, 0, 1]), ([300], [170]), ([1, 200, 1], [90, 900, 2])])
+def test_windows_as_large_as_they_can_be(q, kv, causal, window, dtype, cache):
+    """They hide nothing, also where a sequence has more new tokens than the cache holds."""
+    print(f"case window={window} q={q} kv={kv} causal={causal} {dtype} {cache}", flush=True)
+    c = Case(q, kv, 2, 2, 64, 16, dtype, cache, seed=sum(kv), causal=causal, window=window)
+    c.check(c.run())
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES_AND_CACHES)
 def test_many_sequences(dtype, cache):
     """More sequences than a wavefront has lanes, single tokens and chunks among them, and bounds that are larger than needed."""
     rng = np.random.default_rng(7)
