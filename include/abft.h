@@ -547,9 +547,10 @@ const char *abft_strerror(int code);
 /* Library version, e.g. 100 = 1.0.0. */
 int abft_version(void);
 /* Measurement hook: two hipEvent_t handles (cast to void*) that the following abft_gemm /
- * abft_conv / abft_plan_run calls of the calling host thread record on their stream
- * immediately before and after launching the matrix-product kernel itself (not the
- * checksum pre-pass or the comparison).  NULL, NULL switches it off. */
+ * abft_conv / abft_plan_run / abft_gemm_scaled / abft_linear_scaled calls of the calling host thread record on their
+ * stream immediately before and after launching the matrix-product kernel itself (not the
+ * checksum pre-pass, the comparison or the quantisation, but where the product's kernel quantises its few rows itself, that too).
+ * NULL, NULL switches it off. */
 void abft_set_kernel_events(void *start_event, void *stop_event);
 /* Measurement aid behind the choice of MFMA shape for the 256 x 256 tile (no part of the path, no
  * passage of the paper): one launch of a kernel that only multiplies, from registers -- one

@@ -1538,7 +1538,10 @@ int abft_linear_scaled(int M, int N, int K, const void* X, int64_t ldx, int dtyp
             const bool bytes = rows_off_dwords(w.g, ABFT_I8);
             w.g.A = reinterpret_cast<const char*>(X);
             w.g.lda = ldx;
-            return (dtype == ABFT_F16 ? launch_scaled_few_f16 : launch_scaled_few_bf16)(w.kmode, bytes, w.g, st) == hipSuccess ? ABFT_OK : ABFT_E_HIP;
+            if (g_ev_start && hipEventRecord(g_ev_start, st) != hipSuccess) return ABFT_E_HIP;
+            if ((dtype == ABFT_F16 ? launch_scaled_few_f16 : launch_scaled_few_bf16)(w.kmode, bytes, w.g, st) != hipSuccess) return ABFT_E_HIP;
+            if (g_ev_stop && hipEventRecord(g_ev_stop, st) != hipSuccess) return ABFT_E_HIP;
+            return ABFT_OK;
         }
     }
     if (quantize_rows(M, K, X, ldx, dtype, ws, linear_ld(K), row_scale, st) != hipSuccess) return ABFT_E_HIP;

@@ -317,6 +317,29 @@ def test_few_rows_with_a_report_or_a_planted_fault(M):
     assert not differs.any()
 
 
+@pytest.mark.parametrize("M", [1, 4, 9, 200])
+def test_events_around_the_product(M):
+    """The measurement hook records both events in every form of the call: behind what the stream held when it was made."""
+    N, K = 300, 512
+    p = Product(M, N, K, "f16", B.B_NK, seed=M)
+    x = hard_rows(M, K, p.t, seed=1)
+    n = B.abft_linear_scaled_workspace_bytes(M, N, K, B.THREAD)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    start, stop, made = (torch.cuda.Event(enable_timing=True) for _ in range(3))
+    start.record()
+    stop.record()
+    torch.zeros(1 << 24, device=DEV).sin_()   # (time goes by on the stream)
+    made.record()
+    B.abft_set_kernel_events(start.cuda_event, stop.cuda_event)
+    try:
+        B.abft_linear_scaled(M, N, K, x, K, p.dt, p.Bm, p.ldb, B.B_NK, p.cs, p.bias, B.ACT_NONE, p.C, p.ldc, B.THREAD, workspace=ws, workspace_bytes=n,
+                             fault_flag=p.flag)
+    finally:
+        B.abft_set_kernel_events(None, None)
+    torch.cuda.synchronize()
+    assert made.elapsed_time(start) >= 0 and start.elapsed_time(stop) > 0
+
+
 def test_linear_layer_in_a_graph():
     M, N, K = 24, 256, 384
     p = Product(M, N, K, "bf16", B.B_NK, seed=5)
