@@ -531,7 +531,9 @@ int abft_kv_read(const abft_kv_cache_t *cache /* host */, int tokens, const int6
  *          bytes have to be zero before its first use, and are zero again after every call (of whatever shape); the rest needs
  *          no initialisation.  Calls that share one must be ordered on one stream.
  * The products run on the matrix unit in the type of Q (int8 keys and values are exact there), softmax statistics
- * and sums in fp32; the weights w_j are rounded to the type of Q.  The scheme of this library's products does not extend to these
+ * and sums in fp32; the weights w_j are rounded to the type of Q (fp16: what is below 2^-32 of a row's largest weight, for int8 caches
+ * times its value's scale, vanishes beside its value, not in the sum of weights; int8
+ * values' scales below 2^-64, bf16: 2^-100, are taken for that).  The scheme of this library's products does not extend to these
  * two: they are not checked.  The same call gives the same bits.  A sequence's results do not depend on the other sequences but in
  * where long key ranges are cut, and their sums taken apart: that follows the lengths of all of them. */
 int abft_attention(const abft_kv_cache_t *cache /* host */, int n_seqs, const int32_t *q_start, const int32_t *kv_len,

@@ -3,7 +3,8 @@
 // Row (token, query head) with query q sees some of its sequence's keys and becomes sum_j w_j v_j / sum_j w_j with
 // w_j = 2^(c q.k_j - m), c = scale log2(e), in one pass over the keys: m is a running maximum, and sums that were taken under a
 // smaller one are scaled down when it moves.  m only has to be near the maximum, so it moves when a value passes it by more than
-// 2^8 (the weights stay far inside 16 bits, the sums inside fp32), which after a row's first keys hardly happens.
+// 2^8, which after a row's first keys hardly happens.  Weights of fp16 are kept 2^7 larger than that: up to 2^15, so that what
+// vanishes below the type's smallest value is less than 2^-32 of the largest (2^-25 of it, for each of a million keys, were 3 %).
 //
 // Both products run transposed, S^T = K Q^T and O^T = V^T P^T.  The first leaves in each lane weights of one row (its column)
 // and of keys 4 g .. 4 g + 3 of every eight or sixteen, g the lane's group, and that is what the second takes as its operand
@@ -106,9 +107,12 @@ __device__ __forceinline__ i32x2 read_transposed(const char* p) {
 
 __device__ __forceinline__ float swap_halves(float v) { return __shfl_xor(v, 32); }
 
-// log2 of a value's scale and its inverse (a group of zeros: any scale does; NaN stays)
+// log2 of a value's scale and its inverse (a group of zeros: any scale does; NaN stays).  Smaller scales are taken for the least one: 2^-64,
+// nothing in an output of fp16 (and 2^24 weights of 2^15, each times its inverse, stay inside fp32), or 2^-100 for bf16.
+template <int DT>
 __device__ __forceinline__ void value_scale(float t, float& log2_t, float& inv_t) {
-    t = t < 7.8886091e-31f ? 7.8886091e-31f : t;
+    constexpr float LEAST = DT == DT_F16 ? 0x1p-64f : 0x1p-100f;
+    t = t < LEAST ? LEAST : t;
     log2_t = __builtin_amdgcn_logf(t);
     inv_t = __builtin_amdgcn_rcpf(t);
 }
@@ -125,5 +129,8 @@ __device__ __forceinline__ float2 get_shared(const float* p) {
 
 constexpr float ATTN_NONE = -3.402823466e+38f;   // the running maximum before the first key
 constexpr float ATTN_SLACK = 8.f;                // how far (as powers of two) a value may pass it
+// how far below the running maximum the exponents' base is (see above; 2^15 (1 + rounding) is below fp16's 65504)
+template <int DT>
+constexpr float ATTN_LIFT = DT == DT_F16 ? 7.f : 0.f;
 
 }  // namespace abft

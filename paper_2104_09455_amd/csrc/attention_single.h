@@ -257,7 +257,7 @@ __device__ __forceinline__ void single_tokens(const AttnArgs& p, SingleLds<DP>& 
                     inv[b][r] = 1.f;
                     if constexpr (I8) {
                         float lt;
-                        value_scale(vs[b][r], lt, inv[b][r]);
+                        value_scale<DT>(vs[b][r], lt, inv[b][r]);
                         s[b][r] = __builtin_fmaf(acc[r], ks[b][r] * p.c, lt);
                     } else {
                         s[b][r] = acc[r] * p.c;
@@ -284,8 +284,8 @@ __device__ __forceinline__ void single_tokens(const AttnArgs& p, SingleLds<DP>& 
             }
             float top = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(s[0][0], s[0][1]), __builtin_fmaxf(s[0][2], s[0][3])),
                                         __builtin_fmaxf(__builtin_fmaxf(s[1][0], s[1][1]), __builtin_fmaxf(s[1][2], s[1][3])));
-            if (__any(top - m > ATTN_SLACK)) {
-                top = __builtin_fmaxf(top, __shfl_xor(top, 16));
+            if (__any(top - m > ATTN_SLACK + ATTN_LIFT<DT>)) {
+                top = __builtin_fmaxf(top, __shfl_xor(top, 16)) - ATTN_LIFT<DT>;
                 top = __builtin_fmaxf(__builtin_fmaxf(top, __shfl_xor(top, 32)), m);
                 const float f = __builtin_amdgcn_exp2f(m - top);
                 m = top;

@@ -310,7 +310,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
             float* const f = reinterpret_cast<float*>(ks + KEYS * T::PITCH);
             if (lane < NP * PER) {
                 float log2_t, inv_t;
-                value_scale(kt_reg, log2_t, inv_t);
+                value_scale<DT>(kt_reg, log2_t, inv_t);
                 f[scale_key] = kc_reg * p.c;
                 f[scale_key + KEYS] = log2_t;
             }
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
                     *reinterpret_cast<i32x4*>(vs + i * PASS * T::PITCH + (to ^ (16u * e))) = widen8<DT>(vreg[i][2 * e], vreg[i][2 * e + 1]);
             if (lane < NP * PER) {
                 float log2_t, inv_t;
-                value_scale(vt_reg, log2_t, inv_t);
+                value_scale<DT>(vt_reg, log2_t, inv_t);
                 // (a scale that is NaN makes its key's weight NaN where it is seen, and must not reach other rows as 0 times NaN)
                 reinterpret_cast<float*>(vs + KEYS * T::PITCH)[scale_key] = inv_t == inv_t ? inv_t : 0.f;
             }
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
     for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[b][r] = 0.f;
-    float m = ATTN_NONE, l = 0.f;   // (m: as a power of two)
+    float m = ATTN_NONE, l = 0.f;   // (m: as a power of two, ATTN_LIFT below the running maximum)
 
     // ---- the pieces of a tile's way.  S^T, two blocks of 32 keys; key of register r in block kb: k0 + 32 kb + 8 (r / 4) + 4 h + r % 4
     typedef typename MMA::Acc Scores[2];
@@ -412,8 +412,8 @@ __global__ __launch_bounds__(256, 2) void attn_tile_kernel(const AttnArgs p) {
         return I8 ? top : top * p.c;
     };
     auto move_maximum = [&](float top) {
-        if (__any(top - m > ATTN_SLACK)) {
-            top = __builtin_fmaxf(__builtin_fmaxf(top, swap_halves(top)), m);
+        if (__any(top - m > ATTN_SLACK + ATTN_LIFT<DT>)) {
+            top = __builtin_fmaxf(__builtin_fmaxf(top, swap_halves(top)) - ATTN_LIFT<DT>, m);
             const float f = __builtin_amdgcn_exp2f(m - top);
             m = top;
             l *= f;

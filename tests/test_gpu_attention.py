@@ -331,3 +331,45 @@ def test_many_pieces(q, kv, heads, group, dim, window, dtype, cache):
     # (whoever comes last joins the pieces: always in the same order)
     for _ in range(3):
         assert torch.equal(c.run(), got)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES_AND_CACHES)
+@pytest.mark.parametrize("rows", [1, 60000])
+def test_many_small_weights(rows, dtype, cache):
+    """A million keys of e^-18 (less than 2^-25) of the largest weight each: together 1.6 %, which must not get lost, also where
+    one wavefront goes through all of them (as many rows as fill the chip without dividing the keys).
+
+    Bound, as above but with the roundings of the sums and those of an exponent, which have different sizes, apart:
+    e = 2^-24 (keys / 16 + (dim + 64) (1 + max_j scale sum |q k_j|)); and fp16 weights 2^7 above the largest's, small = 2^-32 sum |v_j|."""
+    dt, t, u, tiny = TYPES[dtype]
+    n, dim, page = 1 << 20, 16, 4096
+    g = torch.Generator(device=DEV).manual_seed(3)
+    k = torch.zeros(n // page, 1, page, dim, device=DEV)
+    k[..., 0] = -6
+    k[5, 0, 77, 0] = 0     # the one key of weight 1
+    v = torch.randint(64, 128, k.shape, device=DEV, generator=g).float()
+    ks = vs = None
+    if cache == "i8":
+        ks, vs = (torch.full(k.shape[:3], step, device=DEV) for step in (1.0, 1 / 128))
+        k, v = k.to(torch.int8), v.to(torch.int8)
+    else:
+        k, v = k.to(t), (v / 128).to(t)
+    q = torch.zeros(rows, dim, dtype=t, device=DEV)
+    q[:, 0] = 3
+    out = torch.empty(rows, dim, dtype=t, device=DEV)
+    table = torch.arange(n // page, dtype=torch.int32, device=DEV)
+    q_start = torch.tensor([0, rows], dtype=torch.int32, device=DEV)
+    kv_len = torch.tensor([n], dtype=torch.int32, device=DEV)
+    handle = B.kv_cache(k, v, ks, vs, B.I8 if cache == "i8" else dt, n // page, page, 1, dim)
+    size = B.abft_attention_workspace_bytes(handle, 1, rows, rows, n, 1, dt)
+    ws = torch.zeros(size, dtype=torch.uint8, device=DEV)
+    B.abft_attention(handle, 1, q_start, kv_len, table, n // page, rows, rows, n, q, dim, 1, dt, 1.0, False, 0, out, dim, workspace=ws, workspace_bytes=size)
+    torch.cuda.synchronize()
+    values = v.double().reshape(n, dim) * (1 / 128 if cache == "i8" else 1)
+    w = torch.exp(3 * k.double().reshape(n, dim)[:, 0])
+    want = (w @ values) / w.sum()
+    e = 2.0 ** -24 * (n / 16 + (dim + 64) * 19)
+    small = 2.0 ** -32 * values.sum(0) if dtype == "f16" else torch.zeros_like(want)
+    err = (out.double() - want).abs()
+    bound = (2 * u + 2 * e) * want + small + tiny
+    assert (err <= bound).all(), float((err / bound).max())
