@@ -441,7 +441,7 @@ void abft_plan_destroy(abft_plan_t *plan);
  * int8: with a = max over the row of |x|,
  *     scale[m] = a / 127 (float),   Q[m][k] = 127 x / a rounded to nearest, halves away from zero
  * exactly (|Q| <= 127).  A row of zeros has the scale 0; a row that holds an infinity or a NaN has the scale NaN and Q = 0, so
- * that what is computed from it is NaN.  Q: M x K int8, ldq >= K.  One launch, no workspace. */
+ * that what is computed from it is NaN.  Q: M x K int8, ldq >= K.  One launch (up to 2^23 rows), no workspace. */
 int abft_quantize_rows(int M, int K, const void *X, int64_t ldx, int dtype, void *Q, int64_t ldq, float *scale,
                        void *stream);
 

@@ -165,8 +165,19 @@ inline hipError_t launch_quantize_rows(const QuantizeArgs& a, hipStream_t stream
     else if (a.K <= 2048) kern = quantize_rows_kernel<DT, 256, 1>;
     else if (a.K <= 8192) kern = quantize_rows_kernel<DT, 256, 4>;
     else kern = quantize_rows_kernel<DT, 256, 0>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)((a.M + rows - 1) / rows)), dim3(256), 0, stream, a);
-    return hipGetLastError();
+    // (a launch holds fewer than 2^32 threads)
+    constexpr long long BLOCKS = 1 << 23;
+    for (long long m = 0; m < a.M; m += BLOCKS * rows) {
+        QuantizeArgs b = a;
+        b.X += m * a.ldx * 2;
+        b.Q += m * a.ldq;
+        b.scale += m;
+        b.M = (int)(a.M - m < BLOCKS * rows ? a.M - m : BLOCKS * rows);
+        hipLaunchKernelGGL(kern, dim3((unsigned)((b.M + rows - 1) / rows)), dim3(256), 0, stream, b);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace abft

@@ -80,6 +80,22 @@ def test_quantised_rows_are_exact(M, K, dtype):
         assert torch.equal(q.double(), want)
 
 
+@pytest.mark.parametrize("K", [1, 9])
+def test_more_rows_than_a_launch_holds(K):
+    """2^26 rows, four a workgroup: more than 2^32 threads."""
+    M = (1 << 26) + 5
+    x = torch.zeros(M, K, dtype=torch.float16, device=DEV)
+    places = [0, 1, (1 << 23) - 1, 1 << 23, (1 << 25) - 1, 1 << 25, M - 6, M - 1]
+    x[places] = torch.randn(len(places), K, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)).to(torch.float16)
+    q = torch.full((M, K), GUARD, dtype=torch.int8, device=DEV)
+    scale = torch.full((M,), -5.0, device=DEV)
+    B.abft_quantize_rows(M, K, x, K, B.F16, q, K, scale)
+    torch.cuda.synchronize()
+    want, want_scale = quantised(x[places])
+    assert torch.equal(q[places].double(), want) and torch.equal(scale[places], want_scale)
+    assert int((scale != 0).sum()) == len(places) and int((q != 0).any(1).sum()) == len(places)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 def test_rows_that_are_not_finite_have_scale_nan(dtype):
     _, t, _, _ = TYPES[dtype]
