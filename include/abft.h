@@ -501,7 +501,7 @@ typedef struct {
  *          in a call.
  *   K, V : token t's heads * head_dim values at K + t * ldk (elements, ldk >= heads * head_dim; any alignment: columns
  *          of a larger product as they are), F16 / BF16; a 16-bit cache takes its own type only (ABFT_E_ENUM).
- * tokens = 0 is a call that does nothing. */
+ * tokens = 0 is a call that does nothing; tokens * heads is below 2^31 (ABFT_E_SHAPE). */
 int abft_kv_write(const abft_kv_cache_t *cache /* host */, int tokens, const int64_t *slots, const void *K, int64_t ldk,
                   const void *V, int64_t ldv, int dtype, void *stream);
 /* The way back: K and V receive the slots' values (integer times scale, rounded to dtype); a slot outside the cache reads

@@ -7,6 +7,8 @@
 // 10.5 us (4.6 and 4.9 TB/s), 16384 18.8 and 18.3 (5.4 and 5.6); 8192 in a 16-bit cache 11.5 and 12.2 (5.9 and 5.5).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "kv_cache.h"
 #include "quantize.h"
 
@@ -20,7 +22,7 @@ struct KvArgs {
     char *K, *V;             // the tokens' values
     const int64_t* slots;
     long long ldk, ldv;      // elements
-    unsigned pairs;          // tokens x heads
+    unsigned pairs;          // tokens x heads of the launch
     int heads, dim, page_size;
     int slots_in_cache;
 };
@@ -113,11 +115,23 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const KvArgs p) {
 }
 
 template <int DT, bool I8, int LANES>
-void launch(bool write, const KvArgs& a, hipStream_t st) {
+hipError_t launch(bool write, const KvArgs& all, int tokens, hipStream_t st) {
     constexpr unsigned PER = 256 / LANES;
-    const dim3 grid((a.pairs + PER - 1) / PER);
-    if (write) hipLaunchKernelGGL((kv_write_kernel<DT, I8, LANES>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((kv_read_kernel<DT, I8, LANES>), grid, dim3(256), 0, st, a);
+    // (a launch holds fewer than 2^32 threads)
+    const int step = std::max((int)((1ll << 31) / LANES / all.heads), 1);
+    for (int t = 0; t < tokens; t += std::min(step, tokens - t)) {
+        KvArgs a = all;
+        a.K += t * a.ldk * 2;
+        a.V += t * a.ldv * 2;
+        a.slots += t;
+        a.pairs = (unsigned)std::min(step, tokens - t) * (unsigned)a.heads;
+        const dim3 grid((a.pairs + PER - 1) / PER);
+        if (write) hipLaunchKernelGGL((kv_write_kernel<DT, I8, LANES>), grid, dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((kv_read_kernel<DT, I8, LANES>), grid, dim3(256), 0, st, a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 int kv_move(bool write, const abft_kv_cache_t* c, int tokens, const int64_t* slots, char* K, long long ldk, char* V, long long ldv,
@@ -134,19 +148,19 @@ int kv_move(bool write, const abft_kv_cache_t* c, int tokens, const int64_t* slo
     a.k = reinterpret_cast<char*>(c->k); a.v = reinterpret_cast<char*>(c->v);
     a.k_scale = c->k_scale; a.v_scale = c->v_scale;
     a.K = K; a.V = V; a.slots = slots; a.ldk = ldk; a.ldv = ldv;
-    a.pairs = (unsigned)tokens * (unsigned)c->heads; a.heads = c->heads; a.dim = c->head_dim; a.page_size = c->page_size;
+    a.pairs = 0; a.heads = c->heads; a.dim = c->head_dim; a.page_size = c->page_size;
     a.slots_in_cache = c->pages * c->page_size;
     const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
     const bool i8 = c->dtype == ABFT_I8, f16 = dtype == ABFT_F16;
     auto of_lanes = [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
-        if (f16) i8 ? launch<DT_F16, true, L>(write, a, st) : launch<DT_F16, false, L>(write, a, st);
-        else i8 ? launch<DT_BF16, true, L>(write, a, st) : launch<DT_BF16, false, L>(write, a, st);
+        if (f16) return i8 ? launch<DT_F16, true, L>(write, a, tokens, st) : launch<DT_F16, false, L>(write, a, tokens, st);
+        return i8 ? launch<DT_BF16, true, L>(write, a, tokens, st) : launch<DT_BF16, false, L>(write, a, tokens, st);
     };
-    if (c->head_dim <= 32) of_lanes(std::integral_constant<int, 4>());
-    else if (c->head_dim <= 64) of_lanes(std::integral_constant<int, 8>());
-    else of_lanes(std::integral_constant<int, 16>());
-    return hipGetLastError() == hipSuccess ? ABFT_OK : ABFT_E_HIP;
+    const hipError_t e = c->head_dim <= 32   ? of_lanes(std::integral_constant<int, 4>())
+                         : c->head_dim <= 64 ? of_lanes(std::integral_constant<int, 8>())
+                                             : of_lanes(std::integral_constant<int, 16>());
+    return e == hipSuccess ? ABFT_OK : ABFT_E_HIP;
 }
 
 }  // namespace

@@ -95,3 +95,30 @@ def test_no_tokens():
     _, _, _, _, cache = make_cache(1, 1, 16, 16, "i8", torch.float16)
     B.abft_kv_write(cache, 0, None, None, 16, None, 16, B.F16)
     B.abft_kv_read(cache, 0, None, None, 16, None, 16, B.F16)
+
+
+def test_more_tokens_than_a_launch_holds():
+    """2^24 tokens of 64 heads, most of them nowhere in the cache: more than 2^32 threads.  (Keys and values share their memory.)"""
+    tokens, heads, dim, page = (1 << 24) + 3, 64, 16, 16
+    row = heads * dim
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 40 GB")
+    x = torch.zeros(tokens, row, dtype=torch.bfloat16, device=DEV)
+    places = torch.tensor([0, (1 << 23) - 1, 1 << 23, tokens - 4, tokens - 1], device=DEV)
+    x[places] = torch.randn(5, row, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1)).to(torch.bfloat16)
+    kept = x[places].clone()
+    k = torch.full((1, heads, page, dim), 3.0, dtype=torch.bfloat16, device=DEV)
+    cache = B.kv_cache(k, k, None, None, B.BF16, 1, page, heads, dim)
+    slots = torch.full((tokens,), -1, dtype=torch.int64, device=DEV)
+    at = torch.tensor([9, 2, 15, 4, 0], device=DEV)
+    slots[places] = at
+    B.abft_kv_write(cache, tokens, slots, x, row, x, row, B.BF16)
+    torch.cuda.synchronize()
+    stored = k[0].transpose(0, 1).reshape(page, row)
+    assert torch.equal(stored[at], kept)
+    assert int((stored != 3.0).any(1).sum()) == 5
+    x.fill_(7.0)
+    B.abft_kv_read(cache, tokens, slots, x, row, x, row, B.BF16)
+    torch.cuda.synchronize()
+    assert torch.equal(x[places], kept)
+    assert int(x[:, ::dim].ne(0).any(1).sum()) == 5
