@@ -523,6 +523,8 @@ int abft_kv_read(const abft_kv_cache_t *cache /* host */, int tokens, const int6
  *   total_q, max_q, max_kv (host): all new tokens; upper bounds of a sequence's new tokens and of kv_len (both set how the
  *          work is divided).  Device values beyond them are cut to them, and page numbers to the cache, so that nothing
  *          outside the buffers is read; rows whose numbers were cut have unspecified values.  max_kv <= 2^24.
+ *          total_q * q_heads and n_seqs * q_heads * (max_kv / 128 + 1) are below 2^31 and, where a sequence may have more than one new
+ *          token, (n_seqs + total_q * q_heads / cache.heads / 128) * cache.heads below about 2^24, a launch's size (ABFT_E_SHAPE).
  *   Q    : total_q rows of q_heads * head_dim values, ldq apart; F16 / BF16, 16-byte aligned rows (ABFT_E_LD, as for the
  *          other leading dimensions); q_heads a multiple of cache.heads.  A 16-bit cache has the type of Q.
  *   O    : the same shape, rows ldo apart, of the type of Q, 8-byte aligned rows.

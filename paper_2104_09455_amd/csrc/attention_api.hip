@@ -27,11 +27,14 @@ constexpr int COMPUTE_UNITS = 256, COUNTERS = COMPUTE_UNITS * 4;
 // launches, 75 in one; 48 single tokens and 512 new ones, 32 heads, int8: 123 / 117, and 127 with twice as many.)
 constexpr int MIXED_GROUPS = COMPUTE_UNITS;
 
+constexpr long long MAX_BLOCKS = (1 << 24) - 1;   // of 256 threads: a launch of 2^32 threads or more wraps, without an error
+
 // How a call's work is divided, from what the host knows of it.
 struct Division {
     int single, single_groups;
     int tiles, tile_split;      // tiles: an upper bound of the row tiles, 0: none can be there; whether their keys may be divided
     size_t off_single_o, off_single_ml, off_tile_o, off_tile_ml, bytes;
+    long long blocks(int heads) const { return single_groups + ((long long)tiles + (tile_split ? tile_more_pieces(heads) : 0)) * heads; }
 };
 Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max_kv, int q_heads) {
     Division d;
@@ -50,7 +53,7 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
         d.single_groups = (int)std::min(most, std::max({heads, std::min(units, 128ll), cdiv(units, 4)}));
     }
     if (tiled) {
-        d.tiles = n + (int)((long long)total_q * group / AttnTile<128>::ROWS);
+        d.tiles = (int)std::min(n + (long long)total_q * group / AttnTile<128>::ROWS, MAX_BLOCKS + 1);
         // (as long as there is a counter for each row tile: with two of them for each workgroup that the chip holds, the rows fill it)
         d.tile_split = d.single_groups + (long long)d.tiles * c->heads <= COUNTERS && max_kv > TILE_MIN_CHUNK * ATTN_BLOCK_KEYS;
     }
@@ -78,8 +81,8 @@ int validate(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max_kv
     if (rc != ABFT_OK) return rc;
     if (n <= 0 || total_q < 0 || max_q < 0 || max_q > total_q || max_kv < 0 || max_kv > MAX_KV) return ABFT_E_SHAPE;
     if (q_heads <= 0 || q_heads % c->heads != 0) return ABFT_E_SHAPE;
-    if ((long long)total_q * q_heads > 0x7fffffffll || (long long)n * q_heads * (max_kv / SINGLE_UNIT + 1) > 0x7fffffffll) return ABFT_E_SHAPE;
-    return ABFT_OK;
+    if ((long long)total_q * q_heads > 0x7fffffffll || (long long)n * q_heads > 0x7fffffffll / (max_kv / SINGLE_UNIT + 1)) return ABFT_E_SHAPE;
+    return divide(c, n, total_q, max_q, max_kv, q_heads).blocks(c->heads) > MAX_BLOCKS ? ABFT_E_SHAPE : ABFT_OK;
 }
 
 }  // namespace

@@ -137,3 +137,18 @@ def test_attention(change, code):
              window=0, O=P, ldo=256, workspace=P, workspace_bytes=1 << 40)
     a.update(change)
     refuses(code, lambda: B.abft_attention(B.kv_cache(**CACHE), stream=0, **a))
+
+
+@pytest.mark.parametrize("change,code", [
+    (dict(), E_WORKSPACE), (dict(n_seqs=1 << 17), E_SHAPE), (dict(n_seqs=1, total_q=(1 << 24) + 1, max_q=1 << 24), E_SHAPE),
+    (dict(n_seqs=1 << 20, q_heads=1 << 30, total_q=1, max_q=1), E_SHAPE), (dict(n_seqs=(1 << 31) - 1, q_heads=(1 << 31) - 128, total_q=1, max_q=1, max_kv=1 << 24), E_SHAPE),
+    (dict(n_seqs=1 << 17, total_q=1 << 17, max_q=1), E_WORKSPACE)])
+def test_attention_larger_than_a_launch(change, code):
+    """2^24 workgroups of row tiles and more are refused (the first and the last are just smaller, and end at the missing workspace)."""
+    a = dict(n_seqs=(1 << 17) - 2100, q_start=P, kv_len=P, block_table=P, ld_table=8, total_q=(1 << 18) - 1, max_q=2, max_kv=100, Q=P, ldq=1 << 40, q_heads=128, dtype=B.BF16,
+             scale=0.1, causal=True, window=0, O=P, ldo=1 << 40, workspace=None, workspace_bytes=0)
+    a.update(change)
+    cache = B.kv_cache(**dict(CACHE, heads=128, head_dim=16))
+    refuses(code, lambda: B.abft_attention(cache, stream=0, **a))
+    if code == E_SHAPE:
+        assert B.abft_attention_workspace_bytes(cache, a["n_seqs"], a["total_q"], a["max_q"], a["max_kv"], a["q_heads"], a["dtype"]) == 0
