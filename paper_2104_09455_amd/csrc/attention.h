@@ -43,7 +43,7 @@ struct AttnArgs {
     int single, single_groups;
     unsigned* counters;                 // one for each of them or of the row tiles below, zero before and after a launch
     float *single_o, *single_ml;
-    // The others: at most `tiles` row tiles; tile_split: their keys may be divided, and the pieces' sums go here, row tiles of the same.
+    // The others: at most `tiles` row tiles; up to tile_split of them their keys may be divided, and the pieces' sums go here, row tiles of the same.
     int tiles, tile_split, tile_counters;   // tile_counters: how many counters are theirs
     float *tile_o, *tile_ml;
 };

@@ -32,7 +32,7 @@ constexpr long long MAX_BLOCKS = (1 << 24) - 1;   // of 256 threads: a launch of
 // How a call's work is divided, from what the host knows of it.
 struct Division {
     int single, single_groups;
-    int tiles, tile_split;      // tiles: an upper bound of the row tiles, 0: none can be there; whether their keys may be divided
+    int tiles, tile_split;      // tiles: an upper bound of the row tiles, 0: none can be there; up to how many of them their keys may be divided
     size_t off_single_o, off_single_ml, off_tile_o, off_tile_ml, bytes;
     long long blocks(int heads) const { return single_groups + ((long long)tiles + (tile_split ? tile_more_pieces(heads) : 0)) * heads; }
 };
@@ -53,9 +53,17 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
         d.single_groups = (int)std::min(most, std::max({heads, std::min(units, 128ll), cdiv(units, 4)}));
     }
     if (tiled) {
-        d.tiles = (int)std::min(n + (long long)total_q * group / AttnTile<128>::ROWS, MAX_BLOCKS + 1);
-        // (as long as there is a counter for each row tile: with two of them for each workgroup that the chip holds, the rows fill it)
-        d.tile_split = d.single_groups + (long long)d.tiles * c->heads <= COUNTERS && max_kv > TILE_MIN_CHUNK * ATTN_BLOCK_KEYS;
+        // Row tiles: at most one more for each sequence that has any than the rows fill (single tokens have none where they have a kernel), at least
+        // what the tokens fill that are not such.
+        const long long rows = (long long)total_q * group, at_most = d.single ? std::min(n, total_q / 2) : n, others = d.single ? std::max(total_q - n, 0) : total_q;
+        d.tiles = (int)std::min(at_most + rows / AttnTile<128>::ROWS, MAX_BLOCKS + 1);
+        const long long least = d.single || (long long)n * max_q != total_q ? cdiv(others * group, AttnTile<128>::ROWS) : n * cdiv((long long)max_q * group, AttnTile<128>::ROWS);
+        // Their keys may be divided as long as there is a counter for each: beyond that two of them for each workgroup that the chip holds fill
+        // it.  How many there are, and so whether, is for the device to see.  (us, 8 heads of 128 read by 4 queries each, int8, as if every
+        // sequence had row tiles of its own / so: 127 single tokens and 512 of 32768 895 / 419, 129 and 16 of 32768 926 / 96, 63 and 1024 of
+        // 8192 250 / 220, 100 and 3 x 300 of 5000 178 / 155; 150 x 2 of 2000, undivided both ways, level.)
+        const int counted = (COUNTERS - d.single_groups) / c->heads;
+        if (least <= counted && max_kv > TILE_MIN_CHUNK * ATTN_BLOCK_KEYS) d.tile_split = std::min(d.tiles, counted);
     }
     size_t at = 0;
     auto take = [&](size_t floats) {
@@ -63,7 +71,7 @@ Division divide(const abft_kv_cache_t* c, int n, int total_q, int max_q, int max
         at = align_up(at + floats * 4, 256);
         return here;
     };
-    const size_t places = (size_t)2 * d.single_groups * group, rows = d.tile_split ? (size_t)(d.tiles + tile_more_pieces(c->heads)) * c->heads * AttnTile<128>::ROWS : 0;
+    const size_t places = (size_t)2 * d.single_groups * group, rows = d.tile_split ? (size_t)(d.tile_split + tile_more_pieces(c->heads)) * c->heads * AttnTile<128>::ROWS : 0;
     if (places + rows == 0) return d;
     // (the counters first, always of one size: calls of different shapes share a workspace)
     take(COUNTERS);

@@ -71,9 +71,9 @@ __device__ __forceinline__ bool find_tile(const AttnArgs& p, int t, int rows, Ti
             work += __shfl_xor(work, d);
             tiles += __shfl_xor(tiles, d);
         }
-        // (more than the host counted, where q_start is not what it has to be: no pieces, since there is no room for theirs)
+        // (more than there are counters and room for: no pieces.  Two row tiles for each workgroup that the chip holds fill it.)
         all_tiles = tiles;
-        if (tiles <= p.tiles) chunk = (int)max((work * p.heads + TILE_SLOTS - 1) / TILE_SLOTS, (unsigned long long)TILE_MIN_CHUNK);
+        if (tiles <= p.tile_split) chunk = (int)max((work * p.heads + TILE_SLOTS - 1) / TILE_SLOTS, (unsigned long long)TILE_MIN_CHUNK);
     }
     int before = 0, tiles_before = 0, groups_before = all_tiles;
     for (int s0 = 0; s0 < p.n_seqs; s0 += 64) {

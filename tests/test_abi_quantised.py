@@ -152,3 +152,12 @@ def test_attention_larger_than_a_launch(change, code):
     refuses(code, lambda: B.abft_attention(cache, stream=0, **a))
     if code == E_SHAPE:
         assert B.abft_attention_workspace_bytes(cache, a["n_seqs"], a["total_q"], a["max_q"], a["max_kv"], a["q_heads"], a["dtype"]) == 0
+
+
+def test_room_for_pieces_beside_many_single_tokens():
+    """127 single tokens and a chunk of 512 over 32768 keys: its 16 row tiles of 8 heads have room for two pieces each at least, since single tokens
+    are no row tiles; 8 prompts of 4096, whose row tiles fill the chip, have none."""
+    cache = B.kv_cache(**dict(CACHE, heads=8, head_dim=128))
+    piece = 128 * 128 * 4
+    assert B.abft_attention_workspace_bytes(cache, 128, 639, 512, 32768, 32, B.F16) >= 2 * 16 * 8 * piece
+    assert B.abft_attention_workspace_bytes(cache, 8, 8 * 4096, 4096, 4096, 32, B.F16) == 0

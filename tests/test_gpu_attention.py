@@ -373,3 +373,15 @@ def test_many_small_weights(rows, dtype, cache):
     err = (out.double() - want).abs()
     bound = (2 * u + 2 * e) * want + small + tiny
     assert (err <= bound).all(), float((err / bound).max())
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES_AND_CACHES)
+@pytest.mark.parametrize("q,kv,heads,group,dim", [
+    ([1] * 127 + [40], [30] * 127 + [9000], 8, 1, 64), ([1] * 150 + [16, 300, 0, 2], [17] * 150 + [7000, 900, 5, 3000], 8, 2, 32), ([33] + [1] * 22, [8000] + [100] * 22, 32, 1, 64),
+    ([2] * 140, [1500] * 140, 8, 1, 16)])
+def test_pieces_beside_many_sequences(q, kv, heads, group, dim, dtype, cache):
+    """Chunks whose keys are divided beside more sequences than there are counters for, were each a row tile; and row tiles beyond the counters."""
+    c = Case(q, kv, heads, group, dim, 64, dtype, cache, seed=12)
+    got = c.run()
+    c.check(got)
+    assert torch.equal(c.run(), got)
