@@ -217,9 +217,12 @@ def _ptr(t) -> Optional[int]:
 
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        # (the handle by itself: the Stream object around it takes 2.7 us to make, as long as a launch)
         import torch
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
+        # (the handle by itself where torch gives it: the Stream object around it takes 2.7 us to make, as long as a launch)
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            return torch.cuda.current_stream().cuda_stream or None
+        return raw(torch.cuda.current_device()) or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None

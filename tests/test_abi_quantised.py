@@ -161,3 +161,14 @@ def test_room_for_pieces_beside_many_single_tokens():
     piece = 128 * 128 * 4
     assert B.abft_attention_workspace_bytes(cache, 128, 639, 512, 32768, 32, B.F16) >= 2 * 16 * 8 * piece
     assert B.abft_attention_workspace_bytes(cache, 8, 8 * 4096, 4096, 4096, 32, B.F16) == 0
+
+
+def test_stream_without_the_raw_handle(monkeypatch):
+    """A torch that does not give the current stream's handle by itself: it is taken from the stream."""
+    import types
+
+    import torch
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=4660))
+    assert B._stream(None) == 4660
+    assert B._stream(7) == 7 and B._stream(0) is None
