@@ -832,8 +832,11 @@ int select_mode(int M, int N, int K, int dt) {
 // The faster protected scheme of a scaled product.  Aligned, the global one wherever 32 x 32 tiles are more than one per compute unit:
 // beyond that the thread-level one forms its checksums on the vector unit of every wavefront (bf16 out, thread-level / global,
 // us: 64 x 4096 x 4096 7.7 / 8.2, 96 rows 13.1 / 9.4, 256 rows 17.3 / 12.4, 1024 46 / 26; 128 x 2048 x 8192 9.9 / 10.7, 192 rows
-// 20.3 / 13.2; 512 x 512 x 512 4.3 / 4.5, 1024 rows 5.7 / 5.1).  Else the global one takes a pass over A, and the intensity decides as
-// ever (511 x 1000 x 2047 9.7 / 17.8).
+// 20.3 / 13.2; 512 x 512 x 512 4.3 / 4.5, 1024 rows 5.7 / 5.1).  Few rows, whole calls with the quantisation, weights from memory: 1 x 8192 x
+// 4096 11.5 / 12.2, 1 x 8224 x 4096 15.3 / 13.7, 4 x 11008 x 4096 16.7 / 15.7, 16 x 14336 x 8192 30.8 / 29.1, 32 x 32000 x 1024 20.0 / 17.2; only
+// where the checksums of very many weights are read for few rows is it the wrong way round: 1 x 32000 x 4096 40.0 / 42.3, 4 x 32000 x
+// 8192 64.8 / 74.0, 64 rows 68.4 / 77.5.  Else the global one takes a pass over A, and the intensity decides as ever (511 x 1000 x 2047
+// 9.7 / 17.8).
 int scaled_select(int M, int N, int K, bool aligned) {
     if (aligned) return cdiv(M, 32) * cdiv(N, 32) > 256 ? ABFT_GLOBAL : ABFT_THREAD;
     return select_mode(M, N, K, ABFT_I8);

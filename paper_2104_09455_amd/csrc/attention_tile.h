@@ -1,7 +1,7 @@
 // Many rows: a workgroup of four wavefronts takes 32 rows each of one sequence and head of the cache (rows are the new
 // tokens' query heads of that head, token by token), and all keys that these rows see, 64 at a time, in 16 bits in LDS.
 // Bound: the softmax's vector work beside the MFMAs, and for little work what a piece costs to begin and to join, about 10 us.  Measured, 8 heads of
-// 128 read by 4 queries each: 8192 of 8192 tokens, bf16, 540 us (1010 TFLOP/s); from an int8 cache, which is widened on the way, fp16 690; 2048 of
+// 128 read by 4 queries each: 8192 of 8192 tokens, bf16, 536 to 558 us (985 to 1025 TFLOP/s); from an int8 cache, which is widened on the way, fp16 690; 2048 of
 // 12000 in a window of 1000, 80 wide, 42.
 #pragma once
 #include "attention.h"

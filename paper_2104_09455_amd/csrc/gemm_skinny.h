@@ -31,8 +31,9 @@ constexpr int skinny_lds_bytes(int tn) { return SKINNY_WAVES * (1 + tn) * 2048; 
 // The loop and the comparison are those of a call without one, and so is every other element.
 // FEW (scaled products): at most SKINNY_FEW rows of A are not there yet: p.A holds 16-bit activations of type OUT, and each workgroup
 // quantises them for itself, into LDS, while its first weights are on their way.  (Quantised by
-// a launch of their own / here, microseconds per call: 1 x 4096 x 4096 6.95 / 5.2, 2 rows 7.0 / 5.6, 4 rows 7.1 / 6.6, 2 x 4096 x 8192 9.5 / 7.9.
-// Rows past four chunks a thread are level, 4 x 4096 x 8192 9.9 / 9.7, and have a launch of their own.)
+// a launch of their own / here, microseconds per call, weights from the last-level cache: 1 x 4096 x 4096 6.6 / 4.7, 2 rows 6.7 / 5.2, 4 rows 7.1 / 6.2, 2 x 4096
+// x 8192 9.1 / 7.6, 1 x 4096 x 16384 18.8 / 14.5; from memory 9.0 / 7.6, 9.2 / 8.1, 9.6 / 9.0, 12.5 / 11.9, 22.5 / 18.3.  Rows past four chunks a thread are
+// level, 4 x 4096 x 8192 9.6 / 9.5, and have a launch of their own.)
 constexpr int SKINNY_FEW = 4, SKINNY_FEW_BYTES = 16 * 1024;
 constexpr int skinny_few_bytes(int rows, int k) { return (k + 127) / 128 * 128 * rows; }   // quantised, in LDS
 // A thread holds four chunks of eight values, 2^lg of each row; whether that is enough for these rows
