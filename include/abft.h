@@ -104,7 +104,14 @@ typedef enum {
     ABFT_GLOBAL_WEIGHTED = 7
 } abft_mode_t;
 /* Activation function a layer applies to its output as it is stored (Sec. 2.4 step 4). */
-typedef enum { ABFT_ACT_NONE = 0, ABFT_ACT_RELU = 1 } abft_act_t;
+typedef enum {
+    ABFT_ACT_NONE = 0,
+    ABFT_ACT_RELU = 1,
+    /* abft_gemm_scaled_add, abft_gemm_gated and their linear forms only, else ABFT_E_ENUM.  NaN stays; -infinity gives 0. */
+    ABFT_ACT_SILU = 2,      /* x / (1 + exp(-x)) */
+    ABFT_ACT_GELU = 3,      /* x Phi(x), the error function's form */
+    ABFT_ACT_GELU_TANH = 4  /* x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
+} abft_act_t;
 
 /* Operand type.  F16 / BF16: A, B and C are fp16 / bf16, accumulation in fp32.
  * I8: A and B are int8, C is int32, accumulation in int32 (exact). */
@@ -477,6 +484,52 @@ int abft_linear_scaled(int M, int N, int K, const void *X, int64_t ldx, int dtyp
                        const abft_fault_t *inject, void *stream);
 /* Bytes of workspace abft_linear_scaled wants (0 for invalid arguments). */
 size_t abft_linear_scaled_workspace_bytes(int M, int N, int K, int mode);
+
+/* ---- what stands between the int8 products of a transformer block -------------- */
+/* Root-mean-square norm of the rows of X (M x K, ldx >= K, F16 or BF16, any alignment), behind the addition of a residual:
+ *     s = x + r, rounded to dtype;   y = s / sqrt(mean over the row of s^2 + eps) * weight, rounded to dtype;
+ *     (q, scale) = what abft_quantize_rows makes of y, bit for bit
+ * The mean is of squares held as floats (rows whose squares pass their range are taken 2^80 smaller; squares below 2^-126 are
+ * zero).  A row that holds an infinity or a NaN gives what the formula gives: NaN for those values (an infinity's other values: 0).
+ *   weight: K floats, or NULL for ones.   eps: finite and above 0 (ABFT_E_VALUE)
+ *   R     : M x K of dtype, ldr >= K, or NULL: s = x
+ *   S     : receives s, lds >= K, or NULL (with R only, else ABFT_E_NULL).  May be X or R (the same rows).
+ *   Y     : receives y, ldy >= K, or NULL.   Q: int8, ldq >= K, and scale: M floats, or both NULL.  At least one of Y and Q
+ *           (ABFT_E_NULL).  They overlap no operand.
+ * One launch (up to 2^23 rows), no workspace. */
+int abft_rms_norm(int M, int K, const void *X, int64_t ldx, int dtype, const float *weight, float eps, const void *R, int64_t ldr,
+                  void *S, int64_t lds, void *Y, int64_t ldy, void *Q, int64_t ldq, float *scale, void *stream);
+
+/* abft_gemm_scaled and abft_linear_scaled with a residual added behind the activation function, in the same kernel:
+ *     C = R + act((A.B) * row_scale * col_scale + bias), one rounding
+ *   R  : M x N, ldr >= N, of the type of C.  May be C itself (the same rows); overlaps it in no other way.
+ *   act: any abft_act_t.
+ * All else, workspaces and the scheme of ABFT_AUTO among it, as there. */
+int abft_gemm_scaled_add(int M, int N, int K, const void *A, int64_t lda, const float *row_scale, const void *B, int64_t ldb,
+                         int b_layout, const float *col_scale, const float *bias, int act, const void *R, int64_t ldr, void *C,
+                         int64_t ldc, int out_dtype, int mode, const void *beta, void *workspace, size_t workspace_bytes,
+                         uint32_t *fault_flag, abft_report_t *report, const abft_fault_t *inject, void *stream);
+int abft_linear_scaled_add(int M, int N, int K, const void *X, int64_t ldx, int dtype, const void *B, int64_t ldb, int b_layout,
+                           const float *col_scale, const float *bias, int act, const void *R, int64_t ldr, void *C, int64_t ldc,
+                           int mode, const void *beta, void *workspace, size_t workspace_bytes, uint32_t *fault_flag,
+                           abft_report_t *report, const abft_fault_t *inject, void *stream);
+
+/* Both projections of a gated feed-forward block, the activation of one and the product of the two, in one kernel:
+ *     C[m][j] = act(z[m][2j]) * z[m][2j + 1],   z = (A.B) * row_scale * col_scale + bias, one rounding
+ *   N  : the columns of C (ldc >= N, up to 2^30 - 1).  B, col_scale and bias have 2N: each gate's in front of its partner's (of
+ *        two N x K matrices in ABFT_B_NK order, rows 2j and 2j + 1 are row j of the first and of the second).
+ *   act: any abft_act_t.
+ * The product that is checked is the one of M x 2N: its regions, tiles, weight checksums, workspace (abft_workspace_bytes,
+ * abft_linear_scaled_workspace_bytes), scheme of ABFT_AUTO and fault descriptors are those of abft_gemm_scaled and
+ * abft_linear_scaled with 2N for N.  All else as there. */
+int abft_gemm_gated(int M, int N, int K, const void *A, int64_t lda, const float *row_scale, const void *B, int64_t ldb,
+                    int b_layout, const float *col_scale, const float *bias, int act, void *C, int64_t ldc, int out_dtype, int mode,
+                    const void *beta, void *workspace, size_t workspace_bytes, uint32_t *fault_flag, abft_report_t *report,
+                    const abft_fault_t *inject, void *stream);
+int abft_linear_gated(int M, int N, int K, const void *X, int64_t ldx, int dtype, const void *B, int64_t ldb, int b_layout,
+                      const float *col_scale, const float *bias, int act, void *C, int64_t ldc, int mode, const void *beta,
+                      void *workspace, size_t workspace_bytes, uint32_t *fault_flag, abft_report_t *report,
+                      const abft_fault_t *inject, void *stream);
 
 /* ---- a paged cache of keys and values, and attention over it ------------------ */
 /* The cache of one attention layer: `pages` pages of `page_size` tokens.  A token's place is a slot,

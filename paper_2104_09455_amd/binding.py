@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libabft.so")
 
 # enums of abft.h
 NONE, GLOBAL, THREAD, AUTO, REPLICA, THREAD_HALF, TWOSIDED, GLOBAL_WEIGHTED = 0, 1, 2, 3, 4, 5, 6, 7
-ACT_NONE, ACT_RELU = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 F16, BF16, I8 = 0, 1, 2
 B_NK, B_KN = 0, 1
 OK = 0
@@ -68,6 +68,7 @@ EXPORTS = [
     "abft_tolerance_half_coeff", "abft_plan_run_chain", "abft_plan_chain_status", "abft_plan_chain_reset",
     "abft_plan_set_diagnostics", "abft_kernel_name", "abft_handover_launches", "abft_chain_launches", "abft_shared_launches", "abft_mfma_probe", "abft_mfma_probe_bytes",
     "abft_quantize_rows", "abft_gemm_scaled", "abft_linear_scaled", "abft_linear_scaled_workspace_bytes", "abft_scaled_select",
+    "abft_rms_norm", "abft_gemm_scaled_add", "abft_linear_scaled_add", "abft_gemm_gated", "abft_linear_gated",
     "abft_kv_write", "abft_kv_read", "abft_attention", "abft_attention_workspace_bytes",
 ]
 
@@ -181,6 +182,18 @@ def lib() -> ctypes.CDLL:
                                      ctypes.POINTER(Fault), vp]
     L.abft_linear_scaled_workspace_bytes.restype = sz
     L.abft_linear_scaled_workspace_bytes.argtypes = [ci, ci, ci, ci]
+    L.abft_gemm_scaled_add.restype = ci
+    L.abft_gemm_scaled_add.argtypes = [ci, ci, ci, vp, i64, vp, vp, i64, ci, vp, vp, ci, vp, i64, vp, i64, ci, ci, vp, vp, sz, vp, vp,
+                                       ctypes.POINTER(Fault), vp]
+    L.abft_linear_scaled_add.restype = ci
+    L.abft_linear_scaled_add.argtypes = [ci, ci, ci, vp, i64, ci, vp, i64, ci, vp, vp, ci, vp, i64, vp, i64, ci, vp, vp, sz, vp, vp,
+                                         ctypes.POINTER(Fault), vp]
+    L.abft_gemm_gated.restype = ci
+    L.abft_gemm_gated.argtypes = L.abft_gemm_scaled.argtypes
+    L.abft_linear_gated.restype = ci
+    L.abft_linear_gated.argtypes = L.abft_linear_scaled.argtypes
+    L.abft_rms_norm.restype = ci
+    L.abft_rms_norm.argtypes = [ci, ci, vp, i64, ci, vp, ctypes.c_float, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp]
     L.abft_scaled_select.restype = ci
     L.abft_scaled_select.argtypes = [ci, ci, ci, ci]
     cp = ctypes.POINTER(KVCache)
@@ -480,6 +493,46 @@ def abft_linear_scaled(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias
     _check(lib().abft_linear_scaled(M, N, K, _ptr(X), ldx, dtype, _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act, _ptr(C),
                                     ldc, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag), _ptr(report), ip,
                                     _stream(stream)))
+
+
+def abft_gemm_scaled_add(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, R, ldr, C, ldc, out_dtype, mode, beta=None,
+                         workspace=None, workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None,
+                         stream=None) -> None:
+    ip = ctypes.byref(inject) if inject is not None else None
+    _check(lib().abft_gemm_scaled_add(M, N, K, _ptr(A), lda, _ptr(row_scale), _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act,
+                                      _ptr(R), ldr, _ptr(C), ldc, out_dtype, mode, _ptr(beta), _ptr(workspace), workspace_bytes,
+                                      _ptr(fault_flag), _ptr(report), ip, _stream(stream)))
+
+
+def abft_linear_scaled_add(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, R, ldr, C, ldc, mode, beta=None, workspace=None,
+                           workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None, stream=None) -> None:
+    ip = ctypes.byref(inject) if inject is not None else None
+    _check(lib().abft_linear_scaled_add(M, N, K, _ptr(X), ldx, dtype, _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act, _ptr(R),
+                                        ldr, _ptr(C), ldc, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag),
+                                        _ptr(report), ip, _stream(stream)))
+
+
+def abft_gemm_gated(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, beta=None,
+                    workspace=None, workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None,
+                    stream=None) -> None:
+    ip = ctypes.byref(inject) if inject is not None else None
+    _check(lib().abft_gemm_gated(M, N, K, _ptr(A), lda, _ptr(row_scale), _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act,
+                                 _ptr(C), ldc, out_dtype, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag),
+                                 _ptr(report), ip, _stream(stream)))
+
+
+def abft_linear_gated(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, C, ldc, mode, beta=None, workspace=None,
+                      workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None, stream=None) -> None:
+    ip = ctypes.byref(inject) if inject is not None else None
+    _check(lib().abft_linear_gated(M, N, K, _ptr(X), ldx, dtype, _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act, _ptr(C),
+                                   ldc, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag), _ptr(report), ip,
+                                   _stream(stream)))
+
+
+def abft_rms_norm(M, K, X, ldx, dtype, weight, eps, residual=None, ldr=0, total=None, ldt=0, Y=None, ldy=0, Q=None, ldq=0, scale=None,
+                  stream=None) -> None:
+    _check(lib().abft_rms_norm(M, K, _ptr(X), ldx, dtype, _ptr(weight), eps, _ptr(residual), ldr, _ptr(total), ldt, _ptr(Y), ldy, _ptr(Q),
+                               ldq, _ptr(scale), _stream(stream)))
 
 
 def abft_scaled_select(M, N, K, aligned=True) -> int:

@@ -724,6 +724,10 @@ struct Problem {
     // scaled int8 product (row_scale not null): the type C is stored in, its scales, a bias or null
     int out_dtype;
     const float *row_scale, *col_scale, *bias;
+    // what its epilogue makes of the scaled values (EPI_*; EPI_GATED: N counts the columns of B, twice those of C), and EPI_ADD's residual
+    int epi;
+    const void* res;
+    long long ldr;
 };
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -908,7 +912,7 @@ int validate_common(const Problem& pr, int mode, const uint32_t* flag) {
     if (mode != ABFT_NONE && !flag) return ABFT_E_NULL;
     if (!pr.conv && pr.lda < pr.K) return ABFT_E_LD;
     if (pr.b_layout == ABFT_B_NK ? pr.ldb < pr.K : pr.ldb < pr.N) return ABFT_E_LD;
-    if (pr.ldc < pr.N) return ABFT_E_LD;
+    if (pr.ldc < (pr.epi == EPI_GATED ? pr.N / 2 : pr.N)) return ABFT_E_LD;
     return ABFT_OK;
 }
 
@@ -1025,21 +1029,33 @@ hipError_t quantize_rows(int M, int K, const void* X, long long ldx, int dtype, 
     a.M = M; a.K = K; a.ldx = ldx; a.ldq = ldq;
     return dtype == ABFT_F16 ? launch_quantize_rows<DT_F16>(a, st) : launch_quantize_rows<DT_BF16>(a, st);
 }
+// What a scaled product's values become (GemmArgs): N counts the columns of C
+struct Epilogue {
+    int epi = EPI_SCALE;
+    const void* res = nullptr;
+    long long ldr = 0;
+};
 // A scaled product as a problem, checked as far as it is more than one in int8; AUTO becomes a scheme.  K: beyond it 128 * 128 * K passes an int32.
 int scaled_problem(int M, int N, int K, const void* A, long long lda, const float* row_scale, const void* B, long long ldb, int b_layout,
                    const float* col_scale, const float* bias, int act, void* C, long long ldc, int out_dtype, int& mode, const uint32_t* flag,
-                   Problem& pr) {
+                   Problem& pr, const Epilogue& to = Epilogue()) {
     std::memset(&pr, 0, sizeof pr);
+    pr.epi = to.epi; pr.res = to.res; pr.ldr = to.ldr;
+    if (to.epi == EPI_GATED) {
+        if (N <= 0 || N > 0x3fffffff) return ABFT_E_SHAPE;
+        N *= 2;
+    }
     pr.M = M; pr.N = N; pr.K = K; pr.dtype = ABFT_I8; pr.b_layout = b_layout;
     pr.A = A; pr.lda = lda; pr.B = B; pr.ldb = ldb; pr.C = C; pr.ldc = ldc;
     pr.act = act; pr.out_dtype = out_dtype;
     pr.row_scale = row_scale; pr.col_scale = col_scale; pr.bias = bias;
     if (out_dtype != ABFT_F16 && out_dtype != ABFT_BF16) return ABFT_E_ENUM;
-    if (act != ABFT_ACT_NONE && act != ABFT_ACT_RELU) return ABFT_E_ENUM;
-    if (!row_scale || !col_scale) return ABFT_E_NULL;
+    if (act < ABFT_ACT_NONE || act > (to.epi == EPI_SCALE ? ABFT_ACT_RELU : ABFT_ACT_GELU_TANH)) return ABFT_E_ENUM;
+    if (!row_scale || !col_scale || (to.epi == EPI_ADD && !to.res)) return ABFT_E_NULL;
     if (K > SCALED_MAX_K) return ABFT_E_SHAPE;
     const int rc = validate_common(pr, mode, flag);
     if (rc != ABFT_OK) return rc;
+    if (to.epi == EPI_ADD && to.ldr < N) return ABFT_E_LD;
     if (mode == ABFT_AUTO) mode = scaled_select(M, N, K, a_vectorisable(pr) && b_vectorisable(pr));
     return mode == ABFT_NONE || mode == ABFT_GLOBAL || mode == ABFT_THREAD ? ABFT_OK : ABFT_E_UNSUPPORTED;
 }
@@ -1107,6 +1123,7 @@ int prepare_problem(const Problem& pr, int mode, const void* beta, void* workspa
     g.flag = flag;
     g.act = pr.act;
     g.row_scale = pr.row_scale; g.col_scale = pr.col_scale; g.bias = pr.bias;
+    g.res = reinterpret_cast<const char*>(pr.res); g.ldr = pr.ldr;
     g.report = reinterpret_cast<Report*>(report);
     const int tol_K = pr.tol_K > 0 ? pr.tol_K : pr.K;
     g.tol_coeff = tol_coeff(tol_K, pr.dtype, mode) + tol_half_coeff(pr.dtype, mode, ci.wm, ci.wn, cfg == CFG_G16 ? 16 : 32);
@@ -1193,6 +1210,20 @@ int prepare_problem(const Problem& pr, int mode, const void* beta, void* workspa
     return ABFT_OK;
 }
 
+// the launches of a scaled product: by what its epilogue makes of the values, and the type they are stored in
+struct ScaledLaunches {
+    hipError_t (*tiles)(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);
+    hipError_t (*skinny)(int mode, bool bytes, int columns, const GemmArgs& args, hipStream_t stream);
+    hipError_t (*few)(int mode, bool bytes, const GemmArgs& args, hipStream_t stream);
+};
+const ScaledLaunches& scaled_launches(const Problem& pr) {
+    static const ScaledLaunches all[3][2] = {
+        {{launch_scaled_f16, launch_scaled_skinny_f16, launch_scaled_few_f16}, {launch_scaled_bf16, launch_scaled_skinny_bf16, launch_scaled_few_bf16}},
+        {{launch_add_f16, launch_add_skinny_f16, launch_add_few_f16}, {launch_add_bf16, launch_add_skinny_bf16, launch_add_few_bf16}},
+        {{launch_gated_f16, launch_gated_skinny_f16, launch_gated_few_f16}, {launch_gated_bf16, launch_gated_skinny_bf16, launch_gated_few_bf16}}};
+    return all[pr.epi][pr.out_dtype == ABFT_F16 ? 0 : 1];
+}
+
 int run_problem(const Problem& pr, int mode, const void* beta, void* workspace, size_t ws_bytes, uint32_t* flag,
                 abft_report_t* report, const abft_fault_t* inject, hipStream_t st) {
     Prepared w;
@@ -1201,9 +1232,9 @@ int run_problem(const Problem& pr, int mode, const void* beta, void* workspace, 
     hipError_t e;
     if (g_ev_start && hipEventRecord(g_ev_start, st) != hipSuccess) return ABFT_E_HIP;
     if (pr.row_scale) {
-        const bool f16 = pr.out_dtype == ABFT_F16;
-        if (w.skinny) e = (f16 ? launch_scaled_skinny_f16 : launch_scaled_skinny_bf16)(w.kmode, rows_off_dwords(w.g, w.dtype), cfg_info_host(w.cfg).wn, w.g, st);
-        else e = f16 ? launch_scaled_f16(w.cfg, w.kmode, w.inj, w.g, st) : launch_scaled_bf16(w.cfg, w.kmode, w.inj, w.g, st);
+        const ScaledLaunches& l = scaled_launches(pr);
+        if (w.skinny) e = l.skinny(w.kmode, rows_off_dwords(w.g, w.dtype), cfg_info_host(w.cfg).wn, w.g, st);
+        else e = l.tiles(w.cfg, w.kmode, w.inj, w.g, st);
     } else if (w.skinny) {
         const int columns = cfg_info_host(w.cfg).wn;
         e = w.dtype == ABFT_F16    ? launch_skinny_f16(w.kmode, rows_off_dwords(w.g, w.dtype), columns, w.g, st)
@@ -1220,6 +1251,43 @@ int run_problem(const Problem& pr, int mode, const void* beta, void* workspace, 
     if (g_ev_stop && hipEventRecord(g_ev_stop, st) != hipSuccess) return ABFT_E_HIP;
 
     return ABFT_OK;
+}
+
+// A linear layer of 16-bit activations: quantised into the workspace, then the product (or both at once)
+int run_linear(int M, int N, int K, const void* X, int64_t ldx, int dtype, const void* B, int64_t ldb, int b_layout, const float* col_scale,
+               const float* bias, int act, const Epilogue& to, void* C, int64_t ldc, int mode, const void* beta, void* workspace,
+               size_t workspace_bytes, uint32_t* fault_flag, abft_report_t* report, const abft_fault_t* inject, void* stream) {
+    int rc = validate_quantize(M, K, X, ldx, dtype);
+    if (rc != ABFT_OK) return rc;
+    const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+    char* const ws = reinterpret_cast<char*>(workspace);
+    const size_t product = linear_product_offset(M, K);
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || workspace_bytes < product) return ABFT_E_WORKSPACE;
+    float* const row_scale = reinterpret_cast<float*>(ws + linear_scale_offset(M, K));
+    Problem pr;
+    rc = scaled_problem(M, N, K, ws, linear_ld(K), row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, dtype, mode, fault_flag, pr, to);
+    if (rc != ABFT_OK) return rc;
+    // (everything that can be refused is, before the first launch)
+    const size_t left = workspace_bytes - product;
+    if (left < plain_workspace_bytes(M, pr.N, K, ABFT_I8, mode)) return ABFT_E_WORKSPACE;
+    if (inject && !inject_in_range(pr, mode, *inject)) return ABFT_E_INJECT;
+    if (skinny_few_fits(M, K) && mode != ABFT_GLOBAL && !report && !inject) {
+        // one launch where the product's kernel can quantise the few rows itself
+        Prepared w;
+        rc = prepare_problem(pr, mode, nullptr, nullptr, 0, fault_flag, nullptr, nullptr, st, w);
+        if (rc != ABFT_OK) return rc;
+        if (w.skinny) {
+            const bool bytes = rows_off_dwords(w.g, ABFT_I8);
+            w.g.A = reinterpret_cast<const char*>(X);
+            w.g.lda = ldx;
+            if (g_ev_start && hipEventRecord(g_ev_start, st) != hipSuccess) return ABFT_E_HIP;
+            if (scaled_launches(pr).few(w.kmode, bytes, w.g, st) != hipSuccess) return ABFT_E_HIP;
+            if (g_ev_stop && hipEventRecord(g_ev_stop, st) != hipSuccess) return ABFT_E_HIP;
+            return ABFT_OK;
+        }
+    }
+    if (quantize_rows(M, K, X, ldx, dtype, ws, linear_ld(K), row_scale, st) != hipSuccess) return ABFT_E_HIP;
+    return run_problem(pr, mode, beta, left ? ws + product : nullptr, left, fault_flag, report, inject, st);
 }
 
 int conv_problem(const abft_conv_t* conv, int N, Problem& pr) {
@@ -1502,6 +1570,28 @@ int abft_gemm_scaled(int M, int N, int K, const void* A, int64_t lda, const floa
     return run_problem(pr, mode, beta, workspace, workspace_bytes, fault_flag, report, inject, reinterpret_cast<hipStream_t>(stream));
 }
 
+int abft_gemm_scaled_add(int M, int N, int K, const void* A, int64_t lda, const float* row_scale, const void* B, int64_t ldb, int b_layout,
+                         const float* col_scale, const float* bias, int act, const void* R, int64_t ldr, void* C, int64_t ldc, int out_dtype,
+                         int mode, const void* beta, void* workspace, size_t workspace_bytes, uint32_t* fault_flag, abft_report_t* report,
+                         const abft_fault_t* inject, void* stream) {
+    Problem pr;
+    const int rc = scaled_problem(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, fault_flag, pr,
+                                  Epilogue{EPI_ADD, R, ldr});
+    if (rc != ABFT_OK) return rc;
+    return run_problem(pr, mode, beta, workspace, workspace_bytes, fault_flag, report, inject, reinterpret_cast<hipStream_t>(stream));
+}
+
+int abft_gemm_gated(int M, int N, int K, const void* A, int64_t lda, const float* row_scale, const void* B, int64_t ldb, int b_layout,
+                    const float* col_scale, const float* bias, int act, void* C, int64_t ldc, int out_dtype, int mode, const void* beta,
+                    void* workspace, size_t workspace_bytes, uint32_t* fault_flag, abft_report_t* report, const abft_fault_t* inject,
+                    void* stream) {
+    Problem pr;
+    const int rc = scaled_problem(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, fault_flag, pr,
+                                  Epilogue{EPI_GATED});
+    if (rc != ABFT_OK) return rc;
+    return run_problem(pr, mode, beta, workspace, workspace_bytes, fault_flag, report, inject, reinterpret_cast<hipStream_t>(stream));
+}
+
 int abft_scaled_select(int M, int N, int K, int aligned) {
     if (M <= 0 || N <= 0 || K <= 0) return ABFT_E_SHAPE;
     return scaled_select(M, N, K, aligned != 0);
@@ -1518,37 +1608,24 @@ int abft_linear_scaled(int M, int N, int K, const void* X, int64_t ldx, int dtyp
                        const float* col_scale, const float* bias, int act, void* C, int64_t ldc, int mode, const void* beta,
                        void* workspace, size_t workspace_bytes, uint32_t* fault_flag, abft_report_t* report, const abft_fault_t* inject,
                        void* stream) {
-    int rc = validate_quantize(M, K, X, ldx, dtype);
-    if (rc != ABFT_OK) return rc;
-    const hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-    char* const ws = reinterpret_cast<char*>(workspace);
-    const size_t product = linear_product_offset(M, K);
-    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || workspace_bytes < product) return ABFT_E_WORKSPACE;
-    float* const row_scale = reinterpret_cast<float*>(ws + linear_scale_offset(M, K));
-    Problem pr;
-    rc = scaled_problem(M, N, K, ws, linear_ld(K), row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, dtype, mode, fault_flag, pr);
-    if (rc != ABFT_OK) return rc;
-    // (everything that can be refused is, before the first launch)
-    const size_t left = workspace_bytes - product;
-    if (left < plain_workspace_bytes(M, N, K, ABFT_I8, mode)) return ABFT_E_WORKSPACE;
-    if (inject && !inject_in_range(pr, mode, *inject)) return ABFT_E_INJECT;
-    if (skinny_few_fits(M, K) && mode != ABFT_GLOBAL && !report && !inject) {
-        // one launch where the product's kernel can quantise the few rows itself
-        Prepared w;
-        rc = prepare_problem(pr, mode, nullptr, nullptr, 0, fault_flag, nullptr, nullptr, st, w);
-        if (rc != ABFT_OK) return rc;
-        if (w.skinny) {
-            const bool bytes = rows_off_dwords(w.g, ABFT_I8);
-            w.g.A = reinterpret_cast<const char*>(X);
-            w.g.lda = ldx;
-            if (g_ev_start && hipEventRecord(g_ev_start, st) != hipSuccess) return ABFT_E_HIP;
-            if ((dtype == ABFT_F16 ? launch_scaled_few_f16 : launch_scaled_few_bf16)(w.kmode, bytes, w.g, st) != hipSuccess) return ABFT_E_HIP;
-            if (g_ev_stop && hipEventRecord(g_ev_stop, st) != hipSuccess) return ABFT_E_HIP;
-            return ABFT_OK;
-        }
-    }
-    if (quantize_rows(M, K, X, ldx, dtype, ws, linear_ld(K), row_scale, st) != hipSuccess) return ABFT_E_HIP;
-    return run_problem(pr, mode, beta, left ? ws + product : nullptr, left, fault_flag, report, inject, st);
+    return run_linear(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, Epilogue(), C, ldc, mode, beta, workspace, workspace_bytes,
+                      fault_flag, report, inject, stream);
+}
+
+int abft_linear_scaled_add(int M, int N, int K, const void* X, int64_t ldx, int dtype, const void* B, int64_t ldb, int b_layout,
+                           const float* col_scale, const float* bias, int act, const void* R, int64_t ldr, void* C, int64_t ldc, int mode,
+                           const void* beta, void* workspace, size_t workspace_bytes, uint32_t* fault_flag, abft_report_t* report,
+                           const abft_fault_t* inject, void* stream) {
+    return run_linear(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, Epilogue{EPI_ADD, R, ldr}, C, ldc, mode, beta, workspace,
+                      workspace_bytes, fault_flag, report, inject, stream);
+}
+
+int abft_linear_gated(int M, int N, int K, const void* X, int64_t ldx, int dtype, const void* B, int64_t ldb, int b_layout,
+                      const float* col_scale, const float* bias, int act, void* C, int64_t ldc, int mode, const void* beta,
+                      void* workspace, size_t workspace_bytes, uint32_t* fault_flag, abft_report_t* report, const abft_fault_t* inject,
+                      void* stream) {
+    return run_linear(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, Epilogue{EPI_GATED}, C, ldc, mode, beta, workspace,
+                      workspace_bytes, fault_flag, report, inject, stream);
 }
 
 size_t abft_static_scratch_bytes(void) { return STATIC_SCRATCH_BYTES; }

@@ -1,0 +1,7 @@
+// Streaming kernel, int8 operands, results scaled to bf16 and added to a residual.
+#define ABFT_DT abft::DT_I8
+#define ABFT_OUT abft::DT_BF16
+#define ABFT_EPI abft::EPI_ADD
+#define ABFT_FAMILY 2
+#define ABFT_LAUNCH_NAME launch_add_stream_bf16
+#include "gemm_launch.inc"

@@ -153,7 +153,16 @@ struct GemmArgs {
     int strip_pitch, strip_rows, strip_seg;
     // scaled int8 products (Cfg::SCALED): one scale per row and per column, and a bias per column or null
     const float *row_scale, *col_scale, *bias;
+    // EPI_ADD: what is added behind the activation function, of the type and shape of C (and C itself, perhaps)
+    const char* res;
+    long long ldr;
 };
+
+// What a scaled product's epilogue makes of its values z (the sums scaled, with their bias):
+//  EPI_SCALE  act(z), none or ReLU
+//  EPI_ADD    act(z) + the residual, any activation function
+//  EPI_GATED  act(z[2j]) * z[2j + 1] for column j of C, which has half the product's columns
+enum { EPI_SCALE = 0, EPI_ADD = 1, EPI_GATED = 2 };
 
 template <typename To, typename Ti>
 __device__ __forceinline__ To bitcast(const Ti& v) {
@@ -296,6 +305,7 @@ struct Cfg {
     static constexpr int ESIZE = (DT_ == DT_I8) ? 1 : 2;  // bytes per input element
     static constexpr int CSIZE = (DT_ == DT_I8) ? 4 : 2;  // bytes per output element
     static constexpr bool SCALED = false;                 // (ScaledCfg)
+    static constexpr int EPI = EPI_SCALE;                 // (ScaledCfg)
     static constexpr int OUT = DT_;                       // the type that 16-bit outputs are stored in
     static constexpr int EPC = 16 / ESIZE;                // elements per 16-byte chunk
     static constexpr int WM = MI_ * TM_, WN = MI_ * TN_;  // wavefront register tile
@@ -322,11 +332,11 @@ struct Cfg {
 // see, exactly) times row_scale[m] times col_scale[n], plus bias[n], after the activation function, rounded once.
 // The sum becomes a float (one rounding beyond 2^24), and takes one scale after the other: their product alone could
 // underflow where the result does not.
-template <class BASE, int OUT_>
+template <class BASE, int OUT_, int EPI_ = EPI_SCALE>
 struct ScaledCfg : BASE {
     static_assert(BASE::DT == DT_I8 && OUT_ != DT_I8, "int8 in, 16 bits out");
     static constexpr bool SCALED = true;
-    static constexpr int OUT = OUT_, CSIZE = 2;
+    static constexpr int OUT = OUT_, CSIZE = 2, EPI = EPI_;
 };
 
 __device__ __forceinline__ i32x4 ld16(const char* p) { return *reinterpret_cast<const i32x4*>(p); }
@@ -349,6 +359,12 @@ __device__ __forceinline__ i32x4 ld16g(const char* p) {
 __device__ __forceinline__ i32x4 shift_down(const i32x4& v, int bytes) {
     unsigned __int128 u = bitcast<unsigned __int128>(v);
     return bitcast<i32x4>(u >> (8 * bytes));
+}
+
+// and up, zeros at the bottom
+__device__ __forceinline__ i32x4 shift_up(const i32x4& v, int bytes) {
+    unsigned __int128 u = bitcast<unsigned __int128>(v);
+    return bitcast<i32x4>(u << (8 * bytes));
 }
 
 // zeros that stand in for rows beyond the matrix edge and for convolution padding
@@ -830,6 +846,62 @@ __device__ __forceinline__ float scaled_value(int sum, float row, float col, flo
     const float v = __builtin_fmaf((float)sum * row, col, bias);
     return act && v < 0.f ? 0.f : v;
 }
+// The activation functions of EPI_ADD and EPI_GATED.  NaN stays in all of them.
+struct ActLinear {   // z, or max(z, 0)
+    bool relu;
+    __device__ __forceinline__ float operator()(float z) const { return relu && z < 0.f ? 0.f : z; }
+};
+// z / (1 + exp(-b z (1 + d z^2))): SiLU (b = 1, d = 0), and GELU's tanh form, z (1 + tanh a) / 2 with a = sqrt(2 / pi) (z + 0.044715 z^3),
+// since (1 + tanh a) / 2 = 1 / (1 + exp(-2 a)).  `linear` and `cubic` are -b and -b d in powers of two.  (z^2 is cut where the
+// function has long been z or 0: beyond it would become infinite, and infinity times d = 0 no number.)
+struct ActSigmoid {
+    float linear, cubic;
+    __device__ __forceinline__ float operator()(float z) const {
+        const float z2 = __builtin_fminf(z * z, 1e12f);
+        const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * __builtin_fmaf(z2, cubic, linear)));
+        return s == 0.f ? 0.f : z * s;   // (so is -infinity)
+    }
+};
+// z Phi(z), GELU itself: Phi(-|z|) = t P(t) exp(-z^2 / 2) with t = 1 / (1 + 0.3 |z|), P of degree 7, fitted to the largest relative error
+// over 0 <= |z| <= 14, 1.5e-7 (beyond it Phi is below 1e-44); no cancellation on either side.
+struct ActGelu {
+    __device__ __forceinline__ float operator()(float z) const {
+        constexpr float P[8] = {0.11962930f, 0.12075396f, 0.09991345f, 0.12856178f, -0.05368396f, 0.20635387f, -0.15720332f, 0.03567483f};
+        const float a = __builtin_fminf(__builtin_fabsf(z), 20.f), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, a, 1.f));
+        float q = P[7];
+#pragma unroll
+        for (int c = 6; c >= 0; --c) q = __builtin_fmaf(q, t, P[c]);
+        const float below = a * q * t * __builtin_amdgcn_exp2f(-0.72134752f * a * a);   // |z| Phi(-|z|)
+        return z < 0.f ? -below : z - below;
+    }
+};
+// f with the activation function `act` (abft_act_t; the same for every lane)
+template <class F>
+__device__ __forceinline__ void with_activation(int act, F f) {
+    constexpr float LOG2E = 1.44269504f, B = 1.59576912f;   // 2 sqrt(2 / pi)
+    if (act <= 1) f(ActLinear{act == 1});
+    else if (act == 3) f(ActGelu{});
+    else f(act == 2 ? ActSigmoid{-LOG2E, 0.f} : ActSigmoid{-LOG2E * B, -LOG2E * B * 0.044715f});
+}
+// EPI_GATED where adjacent lanes hold adjacent columns: `lo` and `hi` are two values of a lane's column, of a row and another.  What
+// the lane makes of them and its neighbour's: the first row's element of C in even lanes, the second's in odd ones.
+template <class ACT>
+__device__ __forceinline__ float gated_pair(float lo, float hi, bool odd, const ACT& act) {
+    const float got = dpp_move<0xB1>(odd ? lo : hi);
+    return act(odd ? got : lo) * (odd ? hi : got);
+}
+// a 16-bit value of type DT at any address, as a float
+template <int DT>
+__device__ __forceinline__ float value16(const char* p) {
+    if constexpr (DT == DT_F16) return (float)*reinterpret_cast<const _Float16*>(p);
+    else return (float)*reinterpret_cast<const __bf16*>(p);
+}
+template <int DT>
+__device__ __forceinline__ void store16(char* p, float v) {
+    if constexpr (DT == DT_F16) *reinterpret_cast<_Float16*>(p) = (_Float16)v;
+    else *reinterpret_cast<__bf16*>(p) = (__bf16)v;
+}
+
 // The scales of up to four consecutive rows; rows outside C take the last one's
 __device__ __forceinline__ f32x4 row_scales(const GemmArgs& p, int row) {
     if (row + 4 <= p.M) return load_global_unaligned<f32x4>(reinterpret_cast<const char*>(p.row_scale + row));
@@ -859,8 +931,110 @@ __device__ __forceinline__ void scale_tile(typename Mma<CFG::DT, CFG::MI>::Acc (
             for (int j = 0; j < CFG::TN; ++j)
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    acc[i][j][r + q] = bitcast<int>(scaled_value(acc[i][j][r + q], row[q], col[j], bias[j], p.act));
+                    acc[i][j][r + q] = bitcast<int>(scaled_value(acc[i][j][r + q], row[q], col[j], bias[j], CFG::EPI == EPI_SCALE ? p.act : 0));
         }
+}
+
+// EPI_ADD: the activation function and the residual, in place (floats already).  Elements outside C take values of its last row or column.
+template <class CFG>
+__device__ __forceinline__ void add_residual(typename Mma<CFG::DT, CFG::MI>::Acc (&acc)[CFG::TM][CFG::TN], const GemmArgs& p,
+                                             const TileCoords<CFG>& tc) {
+    typedef Mma<CFG::DT, CFG::MI> MMA;
+    constexpr int TN = CFG::TN;
+    if (p.act)
+        with_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < CFG::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int r = 0; r < MMA::NACC; ++r) acc[i][j][r] = bitcast<int>(act(bitcast<float>((int)acc[i][j][r])));
+        });
+    const long long ldrb = p.ldr * 2;
+    if constexpr (CFG::INTERLEAVED) {
+        if (tc.bn0 + (tc.wave_n + 1) * CFG::WN <= p.N) {
+            // (a lane's adjacent columns in one load, at whatever address)
+            typedef int Run __attribute__((ext_vector_type(TN / 2)));
+            const char* const from = p.res + (long long)tc.col(0) * 2;
+#pragma unroll
+            for (int i = 0; i < CFG::TM; ++i) {
+                Run v[MMA::NACC];
+#pragma unroll
+                for (int r = 0; r < MMA::NACC; ++r) {
+                    const char* const at = from + min(tc.row(i, r), p.M - 1) * ldrb;
+                    if constexpr (TN == 2) v[r] = ld4u(at);
+                    else v[r] = load_global_unaligned<Run>(at);
+                }
+#pragma unroll
+                for (int r = 0; r < MMA::NACC; ++r)
+#pragma unroll
+                    for (int j = 0; j < TN; j += 2) {
+                        int w;
+                        if constexpr (TN == 2) w = bitcast<int>(v[r]);
+                        else w = v[r][j / 2];
+                        acc[i][j][r] = bitcast<int>(mul_add_half<CFG::OUT, 0>(w, 1.f, bitcast<float>((int)acc[i][j][r])));
+                        acc[i][j + 1][r] = bitcast<int>(mul_add_half<CFG::OUT, 1>(w, 1.f, bitcast<float>((int)acc[i][j + 1][r])));
+                    }
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < CFG::TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const char* const from = p.res + (long long)min(tc.col(j), p.N - 1) * 2;
+            float v[MMA::NACC];
+#pragma unroll
+            for (int r = 0; r < MMA::NACC; ++r) v[r] = value16<CFG::OUT>(from + min(tc.row(i, r), p.M - 1) * ldrb);
+#pragma unroll
+            for (int r = 0; r < MMA::NACC; ++r) acc[i][j][r] = bitcast<int>(bitcast<float>((int)acc[i][j][r]) + v[r]);
+        }
+}
+
+// EPI_GATED: the wavefront tile's elements of C, half as many columns as the product's (floats already), rounded and stored
+template <class CFG>
+__device__ __forceinline__ void store_gated(typename Mma<CFG::DT, CFG::MI>::Acc (&acc)[CFG::TM][CFG::TN], const GemmArgs& p,
+                                            const TileCoords<CFG>& tc) {
+    typedef Mma<CFG::DT, CFG::MI> MMA;
+    constexpr int TN = CFG::TN;
+    auto value = [](int v) { return bitcast<float>(v); };
+    const int cols = p.N / 2;
+    with_activation(p.act, [&](auto act) {
+        if constexpr (CFG::INTERLEAVED) {
+            // both columns of a pair are this lane's
+            const int col = tc.col(0) / 2, left = cols - col;
+            char* const base = p.C + (long long)col * 2;
+#pragma unroll
+            for (int i = 0; i < CFG::TM; ++i)
+#pragma unroll
+                for (int r = 0; r < MMA::NACC; ++r) {
+                    const int row = tc.row(i, r);
+                    const float first = act(value(acc[i][0][r])) * value(acc[i][1][r]);
+                    char* const dst = base + row * p.ldc * 2;
+                    if constexpr (TN == 2) {
+                        if (row < p.M && left > 0) store16<CFG::OUT>(dst, first);
+                    } else {
+                        const int both = pack_out16<CFG::OUT>(first, act(value(acc[i][2][r])) * value(acc[i][3][r]));
+                        struct __attribute__((packed, aligned(2))) Any { int v; };
+                        if (row < p.M && left >= 2) reinterpret_cast<Any*>(dst)->v = both;
+                        else if (row < p.M && left == 1) *reinterpret_cast<short*>(dst) = (short)both;
+                    }
+                }
+        } else {
+            const bool odd = tc.lane & 1;
+#pragma unroll
+            for (int i = 0; i < CFG::TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+#pragma unroll
+                    for (int r = 0; r < MMA::NACC; r += 2) {
+                        const float v = gated_pair(value(acc[i][j][r]), value(acc[i][j][r + 1]), odd, act);
+                        const int row = tc.row(i, r) + (odd ? 1 : 0), col = tc.col(j) / 2;
+                        if (row < p.M && col < cols) store16<CFG::OUT>(p.C + ((long long)row * p.ldc + col) * 2, v);
+                    }
+        }
+    });
 }
 
 // Checksum epilogue (taken from the accumulators, before down-conversion) and store of C.
@@ -1082,6 +1256,11 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
     if (!store) return;
     if constexpr (CFG::SCALED) {
         scale_tile<CFG>(acc, p, tc);
+        if constexpr (CFG::EPI == EPI_ADD) add_residual<CFG>(acc, p, tc);
+        if constexpr (CFG::EPI == EPI_GATED) {
+            store_gated<CFG>(acc, p, tc);
+            return;
+        }
     } else if (p.act) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)

@@ -136,20 +136,24 @@ ABFT_DECLARE_LAUNCHES(bf16)
 ABFT_DECLARE_LAUNCHES(i8)
 #undef ABFT_DECLARE_LAUNCHES
 
-// scaled int8 products: the same per output type, in gemm_scaled_<family>_<type>.hip
-#define ABFT_DECLARE_SCALED(out)                                                                                          \
-    hipError_t launch_scaled_fast_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);    \
-    hipError_t launch_scaled_stream_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);  \
-    hipError_t launch_scaled_generic_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream); \
-    hipError_t launch_scaled_skinny_##out(int mode, bool bytes, int columns, const GemmArgs& args, hipStream_t stream); \
-    hipError_t launch_scaled_few_##out(int mode, bool bytes, const GemmArgs& args, hipStream_t stream);                  \
-    inline hipError_t launch_scaled_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream) {   \
-        if (cfg_is_stream(cfg)) return launch_scaled_stream_##out(cfg, mode, inject, args, stream);                  \
-        if (cfg_is_generic(cfg)) return launch_scaled_generic_##out(cfg, mode, inject, args, stream);                \
-        return launch_scaled_fast_##out(cfg, mode, inject, args, stream);                                            \
+// scaled int8 products: the same per output type and what the epilogue makes of the values, in gemm_<kind>_<family>_<type>.hip
+#define ABFT_DECLARE_SCALED(kind, out)                                                                                     \
+    hipError_t launch_##kind##_fast_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);       \
+    hipError_t launch_##kind##_stream_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);     \
+    hipError_t launch_##kind##_generic_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream);    \
+    hipError_t launch_##kind##_skinny_##out(int mode, bool bytes, int columns, const GemmArgs& args, hipStream_t stream);  \
+    hipError_t launch_##kind##_few_##out(int mode, bool bytes, const GemmArgs& args, hipStream_t stream);                  \
+    inline hipError_t launch_##kind##_##out(int cfg, int mode, bool inject, const GemmArgs& args, hipStream_t stream) {    \
+        if (cfg_is_stream(cfg)) return launch_##kind##_stream_##out(cfg, mode, inject, args, stream);                      \
+        if (cfg_is_generic(cfg)) return launch_##kind##_generic_##out(cfg, mode, inject, args, stream);                    \
+        return launch_##kind##_fast_##out(cfg, mode, inject, args, stream);                                                \
     }
-ABFT_DECLARE_SCALED(f16)
-ABFT_DECLARE_SCALED(bf16)
+ABFT_DECLARE_SCALED(scaled, f16)
+ABFT_DECLARE_SCALED(scaled, bf16)
+ABFT_DECLARE_SCALED(add, f16)
+ABFT_DECLARE_SCALED(add, bf16)
+ABFT_DECLARE_SCALED(gated, f16)
+ABFT_DECLARE_SCALED(gated, bf16)
 #undef ABFT_DECLARE_SCALED
 
 }  // namespace abft

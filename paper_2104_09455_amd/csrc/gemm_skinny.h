@@ -40,7 +40,7 @@ constexpr int skinny_few_bytes(int rows, int k) { return (k + 127) / 128 * 128 *
 constexpr int skinny_few_lg(int k) { return k <= 4096 ? 0 : k <= 8192 ? 1 : 2; }
 constexpr bool skinny_few_fits(int rows, int k) { return rows <= SKINNY_FEW && k <= 16384 && (rows << skinny_few_lg(k)) <= 4; }
 
-template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT, bool FEW = false>
+template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT, bool FEW = false, int EPI = EPI_SCALE>
 __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char* smem) {
     typedef Mma<DT, 16> MMA;
     typedef typename MMA::Acc Acc;
@@ -68,6 +68,12 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
         if constexpr (!FEW) row_scale = row_scales(p, 4 * lgrp);
         col_scale = p.col_scale[n];
         col_bias = p.bias ? p.bias[n] : 0.f;
+    }
+    float res[EPI == EPI_ADD ? 4 : 1];
+    if constexpr (EPI == EPI_ADD) {
+        const char* const from = p.res + (long long)min(n0 + 16 * (TN == 1 ? 0 : wave & 1) + lrow, N - 1) * 2;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) res[r] = value16<OUT>(from + min(4 * lgrp + r, M - 1) * p.ldr * 2);
     }
 
     // Copies: lane l takes chunk l % 8 of rows l / 8 and 8 + l / 8 of a k tile (whole lines; with a lane per row, as the
@@ -298,12 +304,27 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
                 if (col == p.f_col && p.f_row == 4 * lgrp + r) v[r] = p.f_kt == -2 ? flipped : v[r] - part[r] + flipped;
             }
         }
-        if (col < N) {
+        if constexpr (EPI == EPI_GATED) {
+            const bool odd = lane & 1;
+            with_activation(p.act, [&](auto act) {
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    const float g = gated_pair(scaled_value(v[r], row_scale[r], col_scale, col_bias, 0),
+                                               scaled_value(v[r + 1], row_scale[r + 1], col_scale, col_bias, 0), odd, act);
+                    const int row = 4 * lgrp + r + (odd ? 1 : 0);
+                    if (row < M && col < N) store16<OUT>(p.C + ((long long)row * p.ldc + (col >> 1)) * 2, g);
+                }
+            });
+        } else if (col < N) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int row = 4 * lgrp + r;
                 typename std::conditional<SCALED, float, AccT>::type o;
-                if constexpr (SCALED) o = scaled_value(v[r], row_scale[r], col_scale, col_bias, p.act);
+                if constexpr (EPI == EPI_ADD) {
+                    o = scaled_value(v[r], row_scale[r], col_scale, col_bias, 0);
+                    with_activation(p.act, [&](auto act) { o = act(o); });
+                    o += res[r];
+                } else if constexpr (SCALED) o = scaled_value(v[r], row_scale[r], col_scale, col_bias, p.act);
                 else o = p.act ? relu(v[r]) : v[r];
                 if (row < M) {
                     char* const dst = p.C + ((long long)row * p.ldc + col) * (OUT == DT_I8 ? 4 : 2);
@@ -371,12 +392,12 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
     }
 }
 
-template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT, bool FEW = false>
+template <int DT, int TN, int MODE, bool BYTES, bool INJ, int OUT = DT, bool FEW = false, int EPI = EPI_SCALE>
 __global__ __launch_bounds__(64 * SKINNY_WAVES) void gemm_skinny_kernel(const GemmArgs p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     int tile_m, tile_n;
     tile_of_block((int)blockIdx.x, 1, (int)gridDim.x, tile_m, tile_n);   // (a run of columns per die: whole lines of C and A once)
-    skinny_tile<DT, TN, MODE, BYTES, INJ, OUT, FEW>(p, tile_n, smem);
+    skinny_tile<DT, TN, MODE, BYTES, INJ, OUT, FEW, EPI>(p, tile_n, smem);
 }
 
 }  // namespace abft

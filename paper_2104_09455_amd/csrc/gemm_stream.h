@@ -144,6 +144,23 @@ __device__ __forceinline__ void stream_tile(const GemmArgs& p, int tile_m, int t
             col_bias[j] = p.bias ? p.bias[n] : 0.f;
         }
     }
+    // (the residual's rows, two to a register; outside C those of its last row and column)
+    int res[CFG::EPI == EPI_ADD ? CFG::TM * CFG::TN : 1][2];
+    if constexpr (CFG::EPI == EPI_ADD) {
+#pragma unroll
+        for (int i = 0; i < CFG::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < CFG::TN; ++j) {
+                const char* const from = p.res + (long long)min(bn0 + j * 32 + (lane & 31), N - 1) * 2;
+#pragma unroll
+                for (int rr = 0; rr < 4; ++rr) {
+                    const int row = min(bm0 + i * 32 + 8 * (wave & 3) + 4 * (lane >> 5) + rr, M - 1);
+                    const int v = *reinterpret_cast<const unsigned short*>(from + row * p.ldr * 2);
+                    if (rr & 1) res[i * CFG::TN + j][rr >> 1] |= v << 16;
+                    else res[i * CFG::TN + j][rr >> 1] = v;
+                }
+            }
+    }
     constexpr int BETA_ADV = KW * (MDOT ? 128 : BK * 4);
     // first k offset (within a k tile) of the four bytes this lane copies: one float, two halves of a
     // plane, or four digits of a plane
@@ -440,11 +457,35 @@ __device__ __forceinline__ void stream_tile(const GemmArgs& p, int tile_m, int t
             typename std::conditional<CFG::SCALED, float, AccT>::type o[4];
             if constexpr (CFG::SCALED) {
 #pragma unroll
-                for (int rr = 0; rr < 4; ++rr) o[rr] = scaled_value(v[rr], row_scale[i][rr], col_scale[j], col_bias[j], p.act);
+                for (int rr = 0; rr < 4; ++rr)
+                    o[rr] = scaled_value(v[rr], row_scale[i][rr], col_scale[j], col_bias[j], CFG::EPI == EPI_SCALE ? p.act : 0);
             } else {
 #pragma unroll
                 for (int rr = 0; rr < 4; ++rr) o[rr] = (p.act && !(v[rr] > 0)) ? (AccT)0 : v[rr];
             }
+            if constexpr (CFG::EPI == EPI_ADD) {
+                if (p.act)
+                    with_activation(p.act, [&](auto act) {
+#pragma unroll
+                        for (int rr = 0; rr < 4; ++rr) o[rr] = act(o[rr]);
+                    });
+#pragma unroll
+                for (int rr = 0; rr < 4; rr += 2) {
+                    o[rr] = mul_add_half<CFG::OUT, 0>(res[i * TN + j][rr >> 1], 1.f, o[rr]);
+                    o[rr + 1] = mul_add_half<CFG::OUT, 1>(res[i * TN + j][rr >> 1], 1.f, o[rr + 1]);
+                }
+            }
+            if constexpr (CFG::EPI == EPI_GATED) {
+                const bool odd = lane & 1;
+                with_activation(p.act, [&](auto act) {
+#pragma unroll
+                    for (int rr = 0; rr < 4; rr += 2) {
+                        const float g = gated_pair(o[rr], o[rr + 1], odd, act);
+                        const int row = tc.bm0 + i * 32 + 8 * wave + 4 * tc.lgrp + rr + (odd ? 1 : 0);
+                        if (row < M && col < N) store16<CFG::OUT>(p.C + ((long long)row * p.ldc + (col >> 1)) * 2, g);
+                    }
+                });
+            } else {
             if constexpr (CFG::CSIZE == 2) {
                 if (whole) {
                     // rows 8w + 4 (lane / 32) + 0..3 of this block, four columns per lane
@@ -464,6 +505,7 @@ __device__ __forceinline__ void stream_tile(const GemmArgs& p, int tile_m, int t
                         else *reinterpret_cast<int*>(dst) = o[rr];
                     }
                 }
+            }
             }
             if constexpr (CHECKED) {
                 if constexpr (IS_INT) {
