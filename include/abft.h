@@ -504,7 +504,10 @@ int abft_rms_norm(int M, int K, const void *X, int64_t ldx, int dtype, const flo
  *     C = R + act((A.B) * row_scale * col_scale + bias), one rounding
  *   R  : M x N, ldr >= N, of the type of C.  May be C itself (the same rows); overlaps it in no other way.
  *   act: any abft_act_t.
- * All else, workspaces and the scheme of ABFT_AUTO among it, as there. */
+ *   mode: ABFT_AUTO is ABFT_THREAD for up to sixteen rows of weights in ABFT_B_NK order with 16-byte aligned rows (ldb below 2^26) and
+ *        K of 513 .. 16384, a multiple of 16: such products, unprotected or under ABFT_THREAD, have a kernel of their own (which compares
+ *        blocks of 16 x 16; with a report, or a fault at k_after >= 0, they run on the tilings).  Else abft_scaled_select.
+ * All else, workspaces among it, as there. */
 int abft_gemm_scaled_add(int M, int N, int K, const void *A, int64_t lda, const float *row_scale, const void *B, int64_t ldb,
                          int b_layout, const float *col_scale, const float *bias, int act, const void *R, int64_t ldr, void *C,
                          int64_t ldc, int out_dtype, int mode, const void *beta, void *workspace, size_t workspace_bytes,
@@ -520,8 +523,8 @@ int abft_linear_scaled_add(int M, int N, int K, const void *X, int64_t ldx, int 
  *        two N x K matrices in ABFT_B_NK order, rows 2j and 2j + 1 are row j of the first and of the second).
  *   act: any abft_act_t.
  * The product that is checked is the one of M x 2N: its regions, tiles, weight checksums, workspace (abft_workspace_bytes,
- * abft_linear_scaled_workspace_bytes), scheme of ABFT_AUTO and fault descriptors are those of abft_gemm_scaled and
- * abft_linear_scaled with 2N for N.  All else as there. */
+ * abft_linear_scaled_workspace_bytes), scheme of ABFT_AUTO and fault descriptors are those of abft_gemm_scaled_add and
+ * abft_linear_scaled_add with 2N for N.  All else as there. */
 int abft_gemm_gated(int M, int N, int K, const void *A, int64_t lda, const float *row_scale, const void *B, int64_t ldb,
                     int b_layout, const float *col_scale, const float *bias, int act, void *C, int64_t ldc, int out_dtype, int mode,
                     const void *beta, void *workspace, size_t workspace_bytes, uint32_t *fault_flag, abft_report_t *report,

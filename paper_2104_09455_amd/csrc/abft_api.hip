@@ -17,6 +17,7 @@
 
 #include "../../include/abft.h"
 #include "gemm_configs.h"
+#include "gemm_resident.h"
 #include "mlp_chain.h"
 #include "gemm_group.h"
 #include "quantize.h"
@@ -1056,6 +1057,7 @@ int scaled_problem(int M, int N, int K, const void* A, long long lda, const floa
     const int rc = validate_common(pr, mode, flag);
     if (rc != ABFT_OK) return rc;
     if (to.epi == EPI_ADD && to.ldr < N) return ABFT_E_LD;
+    if (mode == ABFT_AUTO && to.epi != EPI_SCALE && b_vectorisable(pr) && resident_fits(M, K) && ldb < (1 << 26)) mode = ABFT_THREAD;
     if (mode == ABFT_AUTO) mode = scaled_select(M, N, K, a_vectorisable(pr) && b_vectorisable(pr));
     return mode == ABFT_NONE || mode == ABFT_GLOBAL || mode == ABFT_THREAD ? ABFT_OK : ABFT_E_UNSUPPORTED;
 }
@@ -1224,6 +1226,37 @@ const ScaledLaunches& scaled_launches(const Problem& pr) {
     return all[pr.epi][pr.out_dtype == ABFT_F16 ? 0 : 1];
 }
 
+// Does the kernel of resident activations take this product?  (its THREAD compares 16 x 16 blocks; a report counts the tilings' own)
+bool resident_takes(const Problem& pr, int mode, const abft_report_t* report, const abft_fault_t* inject) {
+    return pr.epi != EPI_SCALE && (mode == ABFT_NONE || mode == ABFT_THREAD) && b_vectorisable(pr) && resident_fits(pr.M, pr.K) && pr.ldb < (1 << 26) && !report &&
+           (!inject || inject->k_after < 0);
+}
+// x16: activations that are not quantised yet, or null
+int run_resident(const Problem& pr, int mode, const void* x16, long long ldx, uint32_t* flag, const abft_fault_t* inject, hipStream_t st) {
+    GemmArgs g;
+    std::memset(&g, 0, sizeof g);
+    g.A = reinterpret_cast<const char*>(x16 ? x16 : pr.A);
+    g.lda = x16 ? ldx : pr.lda;
+    g.B = reinterpret_cast<const char*>(pr.B);
+    g.C = reinterpret_cast<char*>(pr.C);
+    g.M = pr.M; g.N = pr.N; g.K = pr.K;
+    g.ldb = pr.ldb; g.ldc = pr.ldc;
+    g.flag = flag; g.act = pr.act;
+    g.row_scale = pr.row_scale; g.col_scale = pr.col_scale; g.bias = pr.bias;
+    g.res = reinterpret_cast<const char*>(pr.res); g.ldr = pr.ldr;
+    g.f_row = g.f_col = -1; g.f_kt = -1;
+    if (inject) {
+        if (inject->row < 0 || inject->row >= pr.M || inject->col < 0 || inject->col >= pr.N || inject->bit < 0 || inject->bit > 31 || inject->k_after < -2) return ABFT_E_INJECT;
+        g.f_row = (int)inject->row; g.f_col = (int)inject->col; g.f_bit = inject->bit; g.f_kt = inject->k_after;
+    }
+    const bool f16 = pr.out_dtype == ABFT_F16, checked = mode == ABFT_THREAD;
+    if (g_ev_start && hipEventRecord(g_ev_start, st) != hipSuccess) return ABFT_E_HIP;
+    const hipError_t e = pr.epi == EPI_ADD ? (f16 ? launch_resident_add_f16 : launch_resident_add_bf16)(checked, x16 != nullptr, g, st)
+                                           : (f16 ? launch_resident_gated_f16 : launch_resident_gated_bf16)(checked, x16 != nullptr, g, st);
+    if (e != hipSuccess) return ABFT_E_HIP;
+    return !g_ev_stop || hipEventRecord(g_ev_stop, st) == hipSuccess ? ABFT_OK : ABFT_E_HIP;
+}
+
 int run_problem(const Problem& pr, int mode, const void* beta, void* workspace, size_t ws_bytes, uint32_t* flag,
                 abft_report_t* report, const abft_fault_t* inject, hipStream_t st) {
     Prepared w;
@@ -1271,6 +1304,12 @@ int run_linear(int M, int N, int K, const void* X, int64_t ldx, int dtype, const
     const size_t left = workspace_bytes - product;
     if (left < plain_workspace_bytes(M, pr.N, K, ABFT_I8, mode)) return ABFT_E_WORKSPACE;
     if (inject && !inject_in_range(pr, mode, *inject)) return ABFT_E_INJECT;
+    if (resident_takes(pr, mode, report, inject)) {
+        // (few rows are quantised by the product's own workgroups, each for itself)
+        const bool here = resident_quantises(M, K) && (M <= 4 || M * K <= 49152);
+        if (!here && quantize_rows(M, K, X, ldx, dtype, ws, linear_ld(K), row_scale, st) != hipSuccess) return ABFT_E_HIP;
+        return run_resident(pr, mode, here ? X : nullptr, ldx, fault_flag, inject, st);
+    }
     if (skinny_few_fits(M, K) && mode != ABFT_GLOBAL && !report && !inject) {
         // one launch where the product's kernel can quantise the few rows itself
         Prepared w;
@@ -1578,6 +1617,7 @@ int abft_gemm_scaled_add(int M, int N, int K, const void* A, int64_t lda, const 
     const int rc = scaled_problem(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, fault_flag, pr,
                                   Epilogue{EPI_ADD, R, ldr});
     if (rc != ABFT_OK) return rc;
+    if (resident_takes(pr, mode, report, inject)) return run_resident(pr, mode, nullptr, 0, fault_flag, inject, reinterpret_cast<hipStream_t>(stream));
     return run_problem(pr, mode, beta, workspace, workspace_bytes, fault_flag, report, inject, reinterpret_cast<hipStream_t>(stream));
 }
 
@@ -1589,6 +1629,7 @@ int abft_gemm_gated(int M, int N, int K, const void* A, int64_t lda, const float
     const int rc = scaled_problem(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, fault_flag, pr,
                                   Epilogue{EPI_GATED});
     if (rc != ABFT_OK) return rc;
+    if (resident_takes(pr, mode, report, inject)) return run_resident(pr, mode, nullptr, 0, fault_flag, inject, reinterpret_cast<hipStream_t>(stream));
     return run_problem(pr, mode, beta, workspace, workspace_bytes, fault_flag, report, inject, reinterpret_cast<hipStream_t>(stream));
 }
 

@@ -846,10 +846,11 @@ __device__ __forceinline__ float scaled_value(int sum, float row, float col, flo
     const float v = __builtin_fmaf((float)sum * row, col, bias);
     return act && v < 0.f ? 0.f : v;
 }
-// The activation functions of EPI_ADD and EPI_GATED.  NaN stays in all of them.
-struct ActLinear {   // z, or max(z, 0)
-    bool relu;
-    __device__ __forceinline__ float operator()(float z) const { return relu && z < 0.f ? 0.f : z; }
+// The activation functions of EPI_ADD and EPI_GATED.  NaN stays in all of them.  (No step of them is fused with what follows, or every
+// kernel would round its own way.)
+struct ActLinear {   // z, or max(z, 0): at least `floor`
+    float floor;
+    __device__ __forceinline__ float operator()(float z) const { return z < floor ? floor : z; }
 };
 // z / (1 + exp(-b z (1 + d z^2))): SiLU (b = 1, d = 0), and GELU's tanh form, z (1 + tanh a) / 2 with a = sqrt(2 / pi) (z + 0.044715 z^3),
 // since (1 + tanh a) / 2 = 1 / (1 + exp(-2 a)).  `linear` and `cubic` are -b and -b d in powers of two.  (z^2 is cut where the
@@ -857,6 +858,7 @@ struct ActLinear {   // z, or max(z, 0)
 struct ActSigmoid {
     float linear, cubic;
     __device__ __forceinline__ float operator()(float z) const {
+#pragma clang fp contract(off)
         const float z2 = __builtin_fminf(z * z, 1e12f);
         const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * __builtin_fmaf(z2, cubic, linear)));
         return s == 0.f ? 0.f : z * s;   // (so is -infinity)
@@ -866,6 +868,7 @@ struct ActSigmoid {
 // over 0 <= |z| <= 14, 1.5e-7 (beyond it Phi is below 1e-44); no cancellation on either side.
 struct ActGelu {
     __device__ __forceinline__ float operator()(float z) const {
+#pragma clang fp contract(off)
         constexpr float P[8] = {0.11962930f, 0.12075396f, 0.09991345f, 0.12856178f, -0.05368396f, 0.20635387f, -0.15720332f, 0.03567483f};
         const float a = __builtin_fminf(__builtin_fabsf(z), 20.f), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, a, 1.f));
         float q = P[7];
@@ -879,16 +882,22 @@ struct ActGelu {
 template <class F>
 __device__ __forceinline__ void with_activation(int act, F f) {
     constexpr float LOG2E = 1.44269504f, B = 1.59576912f;   // 2 sqrt(2 / pi)
-    if (act <= 1) f(ActLinear{act == 1});
+    if (act <= 1) f(ActLinear{act == 1 ? 0.f : -__builtin_huge_valf()});
     else if (act == 3) f(ActGelu{});
     else f(act == 2 ? ActSigmoid{-LOG2E, 0.f} : ActSigmoid{-LOG2E * B, -LOG2E * B * 0.044715f});
+}
+// A float as it is: the conversion to 16 bits that follows is not made one with what made it (the instruction for both adds a zero to a
+// product, which takes the sign off another zero; kernels would differ in it)
+__device__ __forceinline__ float as_float(float v) {
+    asm("" : "+v"(v));
+    return v;
 }
 // EPI_GATED where adjacent lanes hold adjacent columns: `lo` and `hi` are two values of a lane's column, of a row and another.  What
 // the lane makes of them and its neighbour's: the first row's element of C in even lanes, the second's in odd ones.
 template <class ACT>
 __device__ __forceinline__ float gated_pair(float lo, float hi, bool odd, const ACT& act) {
     const float got = dpp_move<0xB1>(odd ? lo : hi);
-    return act(odd ? got : lo) * (odd ? hi : got);
+    return as_float(act(odd ? got : lo) * (odd ? hi : got));
 }
 // a 16-bit value of type DT at any address, as a float
 template <int DT>
@@ -988,7 +997,7 @@ __device__ __forceinline__ void add_residual(typename Mma<CFG::DT, CFG::MI>::Acc
 #pragma unroll
             for (int r = 0; r < MMA::NACC; ++r) v[r] = value16<CFG::OUT>(from + min(tc.row(i, r), p.M - 1) * ldrb);
 #pragma unroll
-            for (int r = 0; r < MMA::NACC; ++r) acc[i][j][r] = bitcast<int>(bitcast<float>((int)acc[i][j][r]) + v[r]);
+            for (int r = 0; r < MMA::NACC; ++r) acc[i][j][r] = bitcast<int>(as_float(bitcast<float>((int)acc[i][j][r]) + v[r]));
         }
 }
 
@@ -1010,12 +1019,12 @@ __device__ __forceinline__ void store_gated(typename Mma<CFG::DT, CFG::MI>::Acc 
 #pragma unroll
                 for (int r = 0; r < MMA::NACC; ++r) {
                     const int row = tc.row(i, r);
-                    const float first = act(value(acc[i][0][r])) * value(acc[i][1][r]);
+                    const float first = as_float(act(value(acc[i][0][r])) * value(acc[i][1][r]));
                     char* const dst = base + row * p.ldc * 2;
                     if constexpr (TN == 2) {
                         if (row < p.M && left > 0) store16<CFG::OUT>(dst, first);
                     } else {
-                        const int both = pack_out16<CFG::OUT>(first, act(value(acc[i][2][r])) * value(acc[i][3][r]));
+                        const int both = pack_out16<CFG::OUT>(first, as_float(act(value(acc[i][2][r])) * value(acc[i][3][r])));
                         struct __attribute__((packed, aligned(2))) Any { int v; };
                         if (row < p.M && left >= 2) reinterpret_cast<Any*>(dst)->v = both;
                         else if (row < p.M && left == 1) *reinterpret_cast<short*>(dst) = (short)both;

@@ -156,4 +156,13 @@ ABFT_DECLARE_SCALED(gated, f16)
 ABFT_DECLARE_SCALED(gated, bf16)
 #undef ABFT_DECLARE_SCALED
 
+// products of few rows with their activations in registers (gemm_resident_<kind>_<type>.hip): k tiles of 128 that a wavefront holds, and
+// whether its registers do
+hipError_t launch_resident_add_f16(bool checked, bool from16, const GemmArgs& args, hipStream_t stream);
+hipError_t launch_resident_add_bf16(bool checked, bool from16, const GemmArgs& args, hipStream_t stream);
+hipError_t launch_resident_gated_f16(bool checked, bool from16, const GemmArgs& args, hipStream_t stream);
+hipError_t launch_resident_gated_bf16(bool checked, bool from16, const GemmArgs& args, hipStream_t stream);
+constexpr int resident_tiles(int k) { return k <= 8192 ? (k + 1023) / 1024 : (k + 2047) / 2048 * 2; }
+constexpr bool resident_fits(int rows, int k) { return rows <= 16 && k > 512 && k <= 16384; }
+
 }  // namespace abft

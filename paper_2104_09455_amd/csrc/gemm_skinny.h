@@ -323,7 +323,7 @@ __device__ __forceinline__ void skinny_tile(const GemmArgs& p, int tile_n, char*
                 if constexpr (EPI == EPI_ADD) {
                     o = scaled_value(v[r], row_scale[r], col_scale, col_bias, 0);
                     with_activation(p.act, [&](auto act) { o = act(o); });
-                    o += res[r];
+                    o = as_float(o + res[r]);
                 } else if constexpr (SCALED) o = scaled_value(v[r], row_scale[r], col_scale, col_bias, p.act);
                 else o = p.act ? relu(v[r]) : v[r];
                 if (row < M) {

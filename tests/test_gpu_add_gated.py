@@ -18,6 +18,8 @@ ACTS = [B.ACT_NONE, B.ACT_RELU, B.ACT_SILU, B.ACT_GELU, B.ACT_GELU_TANH]
 
 
 def activated(z, act):
+    if act != B.ACT_NONE:   # (minus infinity's limit, which the formulas do not give)
+        z = torch.where(z == -float("inf"), torch.zeros_like(z), z)
     if act == B.ACT_RELU:
         return torch.where(z < 0, torch.zeros_like(z), z)
     if act == B.ACT_SILU:
@@ -30,6 +32,7 @@ def activated(z, act):
 
 
 def act_error(z, dz, act):
+    z = torch.where(torch.isfinite(z), z, torch.zeros_like(z))   # (infinities go to themselves or to 0)
     own = activated(-z.abs(), act).abs() * (z * z + 8) * 2.0 ** -21 if act > B.ACT_RELU else 0
     return 1.13 * dz + own + activated(z, act).abs() * 2.0 ** -22
 
@@ -94,9 +97,12 @@ class Block(Product):
     def definition(self, act):
         """(values, bounds) in 64 bits."""
         sums = self.a.to(DEV).double() @ self.b.to(DEV).double().t().contiguous()
-        scaled = sums * self.rs.double()[:, None] * self.cs.double()
+        scaled = sums * self.rs.double()[:, None]
+        # (the sum times its row's scale is a float: from 2^128 on, less half a step, infinite)
+        scaled = torch.where(scaled.abs() >= 2.0 ** 128 * (1 - 2.0 ** -25), torch.sign(scaled) * float("inf"), scaled) * self.cs.double()
         z = scaled if self.bias is None else scaled + self.bias.double()
         dz = 2.0 ** -22 * (scaled.abs() + z.abs())
+        dz = torch.where(torch.isfinite(z), dz, torch.zeros_like(dz))   # (infinite is infinite)
         if self.kind == "add":
             y, r = activated(z, act), self.R[:, :self.cols].double()
             want, err = y + r, act_error(z, dz, act) + 2.0 ** -23 * (y.abs() + r.abs())
@@ -109,6 +115,9 @@ class Block(Product):
 
     def check(self, got, act=B.ACT_NONE):
         want, bound = self.definition(act)
+        beyond = ~torch.isfinite(want)
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(got.double()[beyond].nan_to_num(7.0), want[beyond].nan_to_num(7.0))
+        got, want, bound = got[~beyond], want[~beyond], bound[~beyond]
         # (half a step of the type, u times the power of two below its largest value, beyond that value begins infinity)
         top = torch.finfo(self.t).max
         edge = top + self.u * 2.0 ** int(torch.tensor(top).double().log2().floor())
@@ -316,3 +325,59 @@ def test_a_block_as_it_is_used():
         off = (s.double() - last).norm() / last.norm()
         assert off < 2 * u, float(off)
         assert (y.double() - want).norm() / want.norm() < 4 * u
+
+
+# (activations kept in registers: an eighth of k of one to sixteen k tiles a wavefront, k ends inside of a tile and leaves wavefronts without one,
+# columns by the sixteen and by the four, one run of them a workgroup and several, rows quantised by the workgroups and before)
+RESIDENT = [(1, 1, 528), (2, 40, 640), (16, 17, 1024), (3, 700, 1040), (9, 4096, 1408), (1, 12288, 2048), (5, 5000, 3008), (16, 4300, 4096), (1, 8576, 4112), (4, 5120, 5120),
+            (8, 333, 6144), (7, 6000, 7040), (1, 4480, 8192), (4, 4096, 9216), (12, 260, 10240), (4, 4096, 12288), (1, 100, 14000), (2, 700, 16384), (16, 2050, 16384)]
+
+
+@pytest.mark.parametrize("kind", ["add", "gated"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", RESIDENT)
+def test_few_rows_of_large_weights(M, N, K, dtype, kind):
+    act = ACTS[(M + N) % 5]
+    print(f"case few {kind} {M}x{N}x{K} {dtype} act={act}", flush=True)
+    p = Block(kind, M, N, K, dtype, B.B_NK, seed=K + M, bias=M % 2 == 0)
+    p.cs *= 0.3
+    x = torch.zeros(M, K + 3, dtype=p.t, device=DEV)
+    x[:, :K] = hard_rows(M, K, p.t, seed=K)
+    x[:, K:] = float("nan")
+    got = p.linear(x, B.AUTO, act)
+    q, scale = quantised(x[:, :K])
+    p.a, p.rs = q.to(torch.int8).cpu(), scale
+    p.check(got, act)
+    # the same from integers, at any address, in every scheme
+    p.lda = K + 5
+    p.bufs.append(torch.full((M, p.lda), 99, dtype=torch.int8, device=DEV))
+    p.bufs[-1][:, :K] = q.to(torch.int8)
+    p.A = p.bufs[-1].data_ptr()
+    for mode in (B.NONE, B.THREAD, B.AUTO):
+        again, flag = p.run(mode, act, in_place=(kind == "add" and mode == B.THREAD))
+        assert flag == 0 and torch.equal(again.contiguous().view(torch.int16), got.contiguous().view(torch.int16))
+    # a report and the global scheme run on the tilings: the same bits
+    for mode, report in ((B.THREAD, True), (B.GLOBAL, False)):
+        again, flag = p.run(mode, act, report=report)
+        assert flag == 0 and torch.equal(again.contiguous().view(torch.int16), got.contiguous().view(torch.int16))
+    clean = got.contiguous().view(torch.int16).clone()
+    for row, col, bit, after in ((0, 0, 4, -1), (M - 1, p.N - 1, 28, -2), (M // 2, p.N // 2, 9, -1)):
+        bad, flag = p.run(B.THREAD, act, inject=B.Fault(row, col, bit, after))
+        assert flag == 1
+        differs = bad.contiguous().view(torch.int16) != clean
+        differs[row, col // 2 if kind == "gated" else col] = False
+        assert not differs.any()
+
+
+def test_few_rows_whose_values_are_not_finite():
+    """A row with an infinity or a NaN among rows quantised by the workgroups: NaN, the flag stays down, other rows are untouched."""
+    for M, N, K in ((1, 100, 4096), (4, 700, 8192), (9, 50, 1040), (16, 64, 2048)):
+        p = Block("gated", M, N, K, "bf16", B.B_NK, seed=2)
+        x = torch.randn(M, K, generator=torch.Generator().manual_seed(M)).to(p.t).to(DEV)
+        plain = p.linear(x, B.THREAD, B.ACT_SILU).clone()
+        x[M // 2, K - 1] = float("inf")
+        x[M - 1, 0] = float("nan")
+        got = p.linear(x, B.THREAD, B.ACT_SILU)
+        bad = torch.zeros(M, dtype=torch.bool, device=DEV)
+        bad[[M // 2, M - 1]] = True
+        assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], plain[~bad])
