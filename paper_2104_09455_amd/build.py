@@ -26,7 +26,7 @@ FLAGS += os.environ.get("ABFT_EXTRA_HIPCC_FLAGS", "").split()   # e.g. -D switch
 SOURCES = [f"gemm_{family}_{dt}.hip" for family in ("fast", "generic", "stream", "group") for dt in ("f16", "bf16", "i8")]
 SOURCES += [f"gemm_scaled_{family}_{out}.hip" for family in ("generic", "fast", "stream") for out in ("f16", "bf16")]
 SOURCES += [f"gemm_{kind}_{family}_{out}.hip" for kind in ("add", "gated") for family in ("generic", "fast", "stream") for out in ("f16", "bf16")]
-SOURCES += [f"gemm_resident_{kind}_{out}.hip" for kind in ("add", "gated") for out in ("f16", "bf16")]
+SOURCES += [f"gemm_{name}_{kind}_{out}.hip" for name in ("resident", "joint") for kind in ("add", "gated") for out in ("f16", "bf16")]
 SOURCES += ["gemm_strip_f16.hip", "gemm_strip_bf16.hip", "abft_api.hip"] + [f"gemm_skinny_{dt}.hip" for dt in ("f16", "bf16", "i8")]
 SOURCES += ["gemm_scaled_skinny.hip", "gemm_add_skinny.hip", "gemm_gated_skinny.hip", "rms_norm.hip", "kv_cache.hip", "attention_f16.hip", "attention_bf16.hip", "attention_api.hip"]
 

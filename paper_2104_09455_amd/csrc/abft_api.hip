@@ -17,6 +17,7 @@
 
 #include "../../include/abft.h"
 #include "gemm_configs.h"
+#include "gemm_joint.h"
 #include "gemm_resident.h"
 #include "mlp_chain.h"
 #include "gemm_group.h"
@@ -1231,9 +1232,14 @@ bool resident_takes(const Problem& pr, int mode, const abft_report_t* report, co
     return pr.epi != EPI_SCALE && (mode == ABFT_NONE || mode == ABFT_THREAD) && b_vectorisable(pr) && resident_fits(pr.M, pr.K) && pr.ldb < (1 << 26) && !report &&
            (!inject || inject->k_after < 0);
 }
-// x16: activations that are not quantised yet, or null
-int run_resident(const Problem& pr, int mode, const void* x16, long long ldx, uint32_t* flag, const abft_fault_t* inject, hipStream_t st) {
-    GemmArgs g;
+// Does the kernel that quantises and multiplies in one launch take this layer of 16-bit activations?
+bool joint_takes(const Problem& pr, int mode, const abft_report_t* report, const abft_fault_t* inject) {
+    return pr.epi != EPI_SCALE && (mode == ABFT_NONE || mode == ABFT_THREAD || mode == ABFT_AUTO) && pr.K >= 16 && pr.K <= JOINT_MAX_K && pr.ldb < (1 << 26) &&
+           (pr.b_layout == ABFT_B_NK || pr.N >= 4) && cdiv(pr.M, JOINT_M) * cdiv(pr.N, JOINT_N) <= 256 && !report &&
+           (!inject || inject->k_after < 0);
+}
+// What the kernels outside of the tilings are told of a product.  x16: activations that are not quantised yet, or null
+int own_arguments(const Problem& pr, const void* x16, long long ldx, uint32_t* flag, const abft_fault_t* inject, GemmArgs& g) {
     std::memset(&g, 0, sizeof g);
     g.A = reinterpret_cast<const char*>(x16 ? x16 : pr.A);
     g.lda = x16 ? ldx : pr.lda;
@@ -1249,12 +1255,33 @@ int run_resident(const Problem& pr, int mode, const void* x16, long long ldx, ui
         if (inject->row < 0 || inject->row >= pr.M || inject->col < 0 || inject->col >= pr.N || inject->bit < 0 || inject->bit > 31 || inject->k_after < -2) return ABFT_E_INJECT;
         g.f_row = (int)inject->row; g.f_col = (int)inject->col; g.f_bit = inject->bit; g.f_kt = inject->k_after;
     }
-    const bool f16 = pr.out_dtype == ABFT_F16, checked = mode == ABFT_THREAD;
+    return ABFT_OK;
+}
+// a launch between the measurement hook's events
+template <class F>
+int launch_between_events(hipStream_t st, F launch) {
     if (g_ev_start && hipEventRecord(g_ev_start, st) != hipSuccess) return ABFT_E_HIP;
-    const hipError_t e = pr.epi == EPI_ADD ? (f16 ? launch_resident_add_f16 : launch_resident_add_bf16)(checked, x16 != nullptr, g, st)
-                                           : (f16 ? launch_resident_gated_f16 : launch_resident_gated_bf16)(checked, x16 != nullptr, g, st);
-    if (e != hipSuccess) return ABFT_E_HIP;
+    if (launch() != hipSuccess) return ABFT_E_HIP;
     return !g_ev_stop || hipEventRecord(g_ev_stop, st) == hipSuccess ? ABFT_OK : ABFT_E_HIP;
+}
+int run_resident(const Problem& pr, int mode, const void* x16, long long ldx, uint32_t* flag, const abft_fault_t* inject, hipStream_t st) {
+    GemmArgs g;
+    const int rc = own_arguments(pr, x16, ldx, flag, inject, g);
+    if (rc != ABFT_OK) return rc;
+    const bool f16 = pr.out_dtype == ABFT_F16;
+    const auto launch = pr.epi == EPI_ADD ? (f16 ? launch_resident_add_f16 : launch_resident_add_bf16) : (f16 ? launch_resident_gated_f16 : launch_resident_gated_bf16);
+    return launch_between_events(st, [&] { return launch(mode == ABFT_THREAD, x16 != nullptr, g, st); });
+}
+int run_joint(const Problem& pr, int mode, const void* x16, long long ldx, uint32_t* flag, const abft_fault_t* inject, hipStream_t st) {
+    GemmArgs g;
+    const int rc = own_arguments(pr, x16, ldx, flag, inject, g);
+    if (rc != ABFT_OK) return rc;
+    g.tiles_m = (int)cdiv(g.M, JOINT_M);
+    g.tiles_n = (int)cdiv(g.N, JOINT_N);
+    const bool f16 = pr.out_dtype == ABFT_F16;
+    const int layout = pr.b_layout == ABFT_B_KN ? JOINT_KN : ((reinterpret_cast<uintptr_t>(g.B) | (uintptr_t)g.ldb) & 3u) ? JOINT_NK_BYTES : JOINT_NK;
+    const auto launch = pr.epi == EPI_ADD ? (f16 ? launch_joint_add_f16 : launch_joint_add_bf16) : (f16 ? launch_joint_gated_f16 : launch_joint_gated_bf16);
+    return launch_between_events(st, [&] { return launch(layout, mode != ABFT_NONE, g, st); });
 }
 
 int run_problem(const Problem& pr, int mode, const void* beta, void* workspace, size_t ws_bytes, uint32_t* flag,
@@ -1298,6 +1325,7 @@ int run_linear(int M, int N, int K, const void* X, int64_t ldx, int dtype, const
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u) || workspace_bytes < product) return ABFT_E_WORKSPACE;
     float* const row_scale = reinterpret_cast<float*>(ws + linear_scale_offset(M, K));
     Problem pr;
+    const int asked = mode;
     rc = scaled_problem(M, N, K, ws, linear_ld(K), row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, dtype, mode, fault_flag, pr, to);
     if (rc != ABFT_OK) return rc;
     // (everything that can be refused is, before the first launch)
@@ -1325,6 +1353,7 @@ int run_linear(int M, int N, int K, const void* X, int64_t ldx, int dtype, const
             return ABFT_OK;
         }
     }
+    if (joint_takes(pr, asked, report, inject)) return run_joint(pr, asked, X, ldx, fault_flag, inject, st);
     if (quantize_rows(M, K, X, ldx, dtype, ws, linear_ld(K), row_scale, st) != hipSuccess) return ABFT_E_HIP;
     return run_problem(pr, mode, beta, left ? ws + product : nullptr, left, fault_flag, report, inject, st);
 }

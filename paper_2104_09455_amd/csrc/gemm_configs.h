@@ -156,6 +156,12 @@ ABFT_DECLARE_SCALED(gated, f16)
 ABFT_DECLARE_SCALED(gated, bf16)
 #undef ABFT_DECLARE_SCALED
 
+// small linear layers in one launch (gemm_joint_<kind>_<type>.hip; layout: JOINT_*)
+hipError_t launch_joint_add_f16(int layout, bool checked, const GemmArgs& args, hipStream_t stream);
+hipError_t launch_joint_add_bf16(int layout, bool checked, const GemmArgs& args, hipStream_t stream);
+hipError_t launch_joint_gated_f16(int layout, bool checked, const GemmArgs& args, hipStream_t stream);
+hipError_t launch_joint_gated_bf16(int layout, bool checked, const GemmArgs& args, hipStream_t stream);
+
 // products of few rows with their activations in registers (gemm_resident_<kind>_<type>.hip): k tiles of 128 that a wavefront holds, and
 // whether its registers do
 hipError_t launch_resident_add_f16(bool checked, bool from16, const GemmArgs& args, hipStream_t stream);

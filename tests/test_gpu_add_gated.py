@@ -381,3 +381,47 @@ def test_few_rows_whose_values_are_not_finite():
         bad = torch.zeros(M, dtype=torch.bool, device=DEV)
         bad[[M // 2, M - 1]] = True
         assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], plain[~bad])
+
+
+# (one launch that quantises and multiplies: k tiles for one to eight wavefronts, ends of k inside of a chunk, columns that end inside of four, rows
+# and weights at every alignment, both orders; 256 tiles of 32 x 64 and one more)
+@pytest.mark.parametrize("kind", ["add", "gated"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(5, 2, 16), (1, 30, 17), (33, 65, 100), (12, 66, 128), (64, 3, 129), (31, 254, 500), (100, 130, 755), (7, 1000, 1000), (257, 70, 1023), (300, 200, 1024),
+                                   (2048, 127, 64), (2050, 256, 200)])
+def test_small_layers_in_one_launch(M, N, K, dtype, kind):
+    act = ACTS[(M + K) % 5]
+    for layout, pad, offset in ((B.B_NK, 0, 0), (B.B_KN, 0, 0), (B.B_NK, 3, 1), (B.B_KN, 5, 3), (B.B_NK, 2, 2)):
+        print(f"case joint {kind} {M}x{N}x{K} {dtype} layout={layout} pad={pad} act={act}", flush=True)
+        p = Block(kind, M, N, K, dtype, layout, seed=K + M, pad=pad, offset=offset, bias=M % 2 == 0)
+        p.cs *= 0.3
+        x = torch.zeros(M, K + 3, dtype=p.t, device=DEV)
+        x[:, :K] = hard_rows(M, K, p.t, seed=K)
+        x[:, K:] = float("nan")
+        got = p.linear(x, B.AUTO, act).clone()
+        q, scale = quantised(x[:, :K])
+        p.a, p.rs = q.to(torch.int8).cpu(), scale
+        p.check(got, act)
+        assert torch.equal(bits16(p.linear(x, B.NONE, act)), bits16(got))
+        # the global scheme runs on the tilings: the same bits
+        assert torch.equal(bits16(p.linear(x, B.GLOBAL, act)), bits16(got))
+        ws, n = p.workspace(B.THREAD, linear=True)
+        for row, col, bit, after in ((0, 0, 4, -1), (M - 1, p.N - 1, 28, -2), (M // 2, p.N // 2, 9, -1)):
+            out = torch.empty(M, N, dtype=p.t, device=DEV)
+            p.flag.zero_()
+            a = (M, N, K, x, x.stride(0), p.dt, p.Bm, p.ldb, layout, p.cs, p.bias, act)
+            more = dict(workspace=ws, workspace_bytes=n, fault_flag=p.flag, inject=B.Fault(row, col, bit, after))
+            if kind == "add":
+                B.abft_linear_scaled_add(*a, p.R, p.ldr, out, N, B.THREAD, **more)
+            else:
+                B.abft_linear_gated(*a, out, N, B.THREAD, **more)
+            torch.cuda.synchronize()
+            assert int(p.flag.item()) == 1
+            p.flag.zero_()
+            differs = bits16(out) != bits16(got)
+            differs[row, col // 2 if kind == "gated" else col] = False
+            assert not differs.any()
+
+
+def bits16(x):
+    return x.contiguous().view(torch.int16)
