@@ -221,21 +221,31 @@ def _check(rc: int) -> None:
 
 def _ptr(t) -> Optional[int]:
     """Device pointer of a torch tensor (or pass an int / None through)."""
-    if t is None:
-        return None
-    if isinstance(t, int):
+    if t is None or isinstance(t, int):
         return t
     return t.data_ptr()
 
 
+_current_stream = None
+
+
+def _find_current_stream():
+    """How the current stream's handle is asked for, looked up once."""
+    import torch
+    # (the handle by itself where torch gives it: the Stream object around it takes 2.7 us to make, as long as a launch)
+    raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+    if raw is None or device is None:
+        return lambda: torch.cuda.current_stream().cuda_stream
+    torch.cuda.init()
+    return lambda: raw(device())
+
+
 def _stream(stream) -> Optional[int]:
     if stream is None:
-        import torch
-        # (the handle by itself where torch gives it: the Stream object around it takes 2.7 us to make, as long as a launch)
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        if raw is None:
-            return torch.cuda.current_stream().cuda_stream or None
-        return raw(torch.cuda.current_device()) or None
+        global _current_stream
+        if _current_stream is None:
+            _current_stream = _find_current_stream()
+        return _current_stream() or None
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
