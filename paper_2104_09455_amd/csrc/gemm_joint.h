@@ -49,8 +49,9 @@ __global__ __launch_bounds__(64 * JOINT_WAVES, 4) void gemm_joint_kernel(const G
 
     // ---- weights: the k tile of 64 columns in 32 registers (off the dword: 40)
     struct Tile {
-        i32x4 v[8];
+        i32x4 v[KN ? 1 : 8];
         int more[BYTES ? 8 : 1];
+        int row[KN ? 32 : 1];   // K x N: four columns of k = 64 s + 16 lgrp + e at 16 s + e
     };
     // N x K: load q covers rows 8 (q % 2) + crow of turn q / 2, whose row r is column 4 r + q / 2.  Columns outside take the last one's weights,
     // and their sums are not stored.
@@ -72,14 +73,14 @@ __global__ __launch_bounds__(64 * JOINT_WAVES, 4) void gemm_joint_kernel(const G
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) t.v[4 * s + (e >> 2)][e & 3] = ld4u(base + (long long)(kt * 128 + s * 64 + e) * p.ldb + mine);
+                    for (int e = 0; e < 16; ++e) t.row[16 * s + e] = ld4u(base + (long long)(kt * 128 + s * 64 + e) * p.ldb + mine);
             } else {
                 // (rows beyond K, multiplied with zeros: the last one again)
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        t.v[4 * s + (e >> 2)][e & 3] = ld4u(base + (long long)min(kt * 128 + s * 64 + lgrp * 16 + e, K - 1) * p.ldb + at_col);
+                        t.row[16 * s + e] = ld4u(base + (long long)min(kt * 128 + s * 64 + lgrp * 16 + e, K - 1) * p.ldb + at_col);
             }
         } else {
             // (chunks beyond K, multiplied with zeros, and one that K cuts: the last 16 bytes of the row)
@@ -141,9 +142,7 @@ __global__ __launch_bounds__(64 * JOINT_WAVES, 4) void gemm_joint_kernel(const G
         if constexpr (KN) {
             if (bn0 + JOINT_N > N) {
 #pragma unroll
-                for (int q = 0; q < 8; ++q)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d) t.v[q][d] = (int)((unsigned)t.v[q][d] >> (8 * over));
+                for (int e = 0; e < 32; ++e) t.row[e] = (int)((unsigned)t.row[e] >> (8 * over));
             }
         }
         i32x4 a[2][2];
@@ -162,8 +161,8 @@ __global__ __launch_bounds__(64 * JOINT_WAVES, 4) void gemm_joint_kernel(const G
 #pragma unroll
                     for (int d = 0; d < 4; ++d) {
                         const unsigned sel = 0x04000400u + 0x01010101u * (unsigned)j;
-                        const unsigned lo = __builtin_amdgcn_perm((unsigned)t.v[4 * s + d][1], (unsigned)t.v[4 * s + d][0], sel);
-                        const unsigned hi = __builtin_amdgcn_perm((unsigned)t.v[4 * s + d][3], (unsigned)t.v[4 * s + d][2], sel);
+                        const unsigned lo = __builtin_amdgcn_perm((unsigned)t.row[16 * s + 4 * d + 1], (unsigned)t.row[16 * s + 4 * d], sel);
+                        const unsigned hi = __builtin_amdgcn_perm((unsigned)t.row[16 * s + 4 * d + 3], (unsigned)t.row[16 * s + 4 * d + 2], sel);
                         w[s][d] = (int)__builtin_amdgcn_perm(hi, lo, 0x05040100u);
                     }
             } else {

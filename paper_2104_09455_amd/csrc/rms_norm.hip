@@ -1,7 +1,9 @@
 // Root-mean-square norm of rows, with the residual's addition before it and, behind it, 16-bit values, int8 with a scale per row, or both:
 //   s = round(x + r),   y = round(s / sqrt(mean s^2 + eps) * w),   (q, scale) = y quantised as abft_quantize_rows does
 // A row stays in its threads' registers from the sum to the integers, so every value is read and written once.
-// Bound: bytes, 2 K each for x, r, s and y; few rows: a chain of two round trips to memory and two sums over the row.
+// Bound: bytes, 2 K each for x, r, s and y; few rows: a chain of two round trips to memory and two sums over the row.  Measured, bf16, with a
+// residual, both of s and y: 8192 x 8192 95.8 us (5.6 TB/s), 4096 x 4096 25.3, 600 x 5000 7.5, 1 x 4096 3.7 in a graph.  Rows at odd addresses: 1861 x 3789
+// 16.8, where the vector memory path takes 16 bytes a lane off the dword at a quarter of its rate.
 #include <hip/hip_runtime.h>
 
 #include "../../include/abft.h"
@@ -22,8 +24,10 @@ struct NormArgs {
     float eps;
 };
 
-struct __attribute__((packed)) AnyChunk { i32x4 v; };
-struct __attribute__((packed)) AnyHalf { i32x2 v; };
+// (results leave past the L2, which the rows on their way in then have for themselves: 8192 x 8192 98.9 -> 95.8 us, 8192 x 5120 63.4 -> 59.7, 600 x 5000
+// 9.3 -> 7.5, few rows level)
+typedef int AnyChunk __attribute__((ext_vector_type(4), aligned(2)));
+typedef int AnyHalf __attribute__((ext_vector_type(2), aligned(1)));
 
 template <int DT>
 __device__ __forceinline__ void unpack(const i32x4& v, float (&f)[8]) {
@@ -51,14 +55,14 @@ __device__ __forceinline__ float square_chunk(const i32x4& v, float lift, float 
     for (int e = 0; e < 8; ++e) sum = __builtin_fmaf(f[e] * lift, f[e] * lift, sum);
     return sum;
 }
-// the first n bytes' worth of a chunk of 16-bit values, n of them (8: all)
+// the first n values of a chunk (8: all)
 __device__ __forceinline__ void store_chunk(char* to, const i32x4& v, int n) {
-    if (n >= 8) reinterpret_cast<AnyChunk*>(to)->v = v;
+    if (n >= 8) __builtin_nontemporal_store(v, reinterpret_cast<AnyChunk*>(to));
     else
         for (int e = 0; e < n; ++e) reinterpret_cast<short*>(to)[e] = (short)(v[e >> 1] >> (16 * (e & 1)));
 }
 __device__ __forceinline__ void store_integers(signed char* to, const i32x2& q, int n) {
-    if (n >= 8) reinterpret_cast<AnyHalf*>(to)->v = q;
+    if (n >= 8) __builtin_nontemporal_store(q, reinterpret_cast<AnyHalf*>(to));
     else
         for (int e = 0; e < n; ++e) to[e] = (signed char)(q[e >> 2] >> (8 * (e & 3)));
 }
@@ -202,10 +206,95 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(const NormArgs p) {
     }
 }
 
+// Many rows of up to 2048 NV values: a workgroup goes from row to row, the weights in its registers and the next row on its way
+template <int DT, int NV>
+__global__ __launch_bounds__(256) void rms_norm_rows_kernel(const NormArgs p) {
+    __shared__ float sums[2][4];
+    __shared__ unsigned tops[2][4];
+    const int tid = threadIdx.x, K = p.K;
+    float w[NV][8];
+    i32x4 a[NV], b[NV];
+    auto load = [&](long long m) {
+        const char *const x = p.X + m * p.ldx * 2, *const r = p.R ? p.R + m * p.ldr * 2 : nullptr;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int k = (c * 256 + tid) * 8;
+            a[c] = k < K ? row_chunk16(x, k, K) : i32x4{0, 0, 0, 0};
+            if (r) b[c] = k < K ? row_chunk16(r, k, K) : i32x4{0, 0, 0, 0};
+        }
+    };
+    load(blockIdx.x);
+#pragma unroll
+    for (int c = 0; c < NV; ++c) weights(p.weight, min((c * 256 + tid) * 8, K - 1), K, w[c]);
+    int buf = 0;
+    for (long long m = blockIdx.x; m < p.M; m += gridDim.x, buf ^= 1) {
+        char *const s = p.S ? p.S + m * p.lds * 2 : nullptr, *const y = p.Y ? p.Y + m * p.ldy * 2 : nullptr;
+        i32x4 v[NV];
+        float total = 0.f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int k = (c * 256 + tid) * 8;
+            v[c] = p.R ? add_chunk<DT>(a[c], b[c]) : a[c];
+            if (s && k < K) store_chunk(s + 2ll * k, v[c], K - k);
+            total = square_chunk<DT>(v[c], 1.f, total);
+        }
+        if (m + gridDim.x < p.M) load(m + gridDim.x);
+        total = wave_sum(total);
+        if ((tid & 63) == 0) sums[buf][tid >> 6] = total;
+        __syncthreads();
+        total = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
+        float lift = 1.f;
+        if (DT == DT_BF16 && !(total < __builtin_huge_valf())) {
+            lift = 0x1p-80f;
+            total = 0.f;
+#pragma unroll
+            for (int c = 0; c < NV; ++c) total = square_chunk<DT>(v[c], lift, total);
+            total = wave_sum(total);
+            __syncthreads();   // (everyone has read the first sums)
+            if ((tid & 63) == 0) sums[buf][tid >> 6] = total;
+            __syncthreads();
+            total = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
+        }
+        const float inv = 1.f / __builtin_sqrtf(total / (float)K + p.eps * (lift * lift));
+        int top = 0;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int k = (c * 256 + tid) * 8;
+            if (k < K) {
+                v[c] = norm_chunk<DT>(v[c], lift, inv, w[c]);
+                if (K - k < 8) v[c] = shift_down(shift_up(v[c], 2 * (8 - (K - k))), 2 * (8 - (K - k)));
+                if (y) store_chunk(y + 2ll * k, v[c], K - k);
+            }
+            top = chunk_magnitude(v[c], top);
+        }
+        if (!p.Q) continue;
+        unsigned best = wave_max(max((unsigned)top & 0xffffu, (unsigned)top >> 16));
+        if ((tid & 63) == 0) tops[buf][tid >> 6] = best;
+        __syncthreads();
+        best = max(max(tops[buf][0], tops[buf][1]), max(tops[buf][2], tops[buf][3]));
+        const GroupScale g = group_scale<DT>(best);
+        if (tid == 0) p.scale[m] = g.scale;
+        signed char* const q = p.Q + m * p.ldq;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            const int k = (c * 256 + tid) * 8;
+            if (k < K) store_integers(q + k, quantize_chunk<DT>(v[c], g), K - k);
+        }
+    }
+}
+
 template <int DT>
 hipError_t launch(const NormArgs& a, hipStream_t stream) {
     void (*kern)(const NormArgs);
     int rows = 1;
+    // (a workgroup for each row / rows in turn, us, bf16 with a residual: 8192 x 8192 105 / 98.7, 8192 x 5120 65 / 63, 4096 x 4096 28.5 / 25.5, 2048 x 4096 15.4 / 15.0,
+    // 1024 x 8192 16.1 / 15.2; 8192 x 2048 25.2 / 26.2, 8192 x 1024 15.2 / 17.3)
+    const int nv = (a.K + 2047) / 2048, wgs = nv == 2 ? 1024 : 512;   // (as many as their registers let the chip hold)
+    if (nv >= 2 && nv <= 4 && a.M >= 2 * wgs) {
+        kern = nv == 2 ? rms_norm_rows_kernel<DT, 2> : nv == 3 ? rms_norm_rows_kernel<DT, 3> : rms_norm_rows_kernel<DT, 4>;
+        hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), 0, stream, a);
+        return hipGetLastError();
+    }
     if (a.K <= 512) { kern = rms_norm_kernel<DT, 64, 1>; rows = 4; }
     else if (a.K <= 2048 && a.M >= 1024) { kern = rms_norm_kernel<DT, 64, 4>; rows = 4; }
     else if (a.K <= 2048) kern = rms_norm_kernel<DT, 256, 1>;

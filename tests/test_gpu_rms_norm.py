@@ -83,7 +83,8 @@ def run(x, dtype, K, residual=None, weight=None, eps=EPS, total=None, y=True, q=
 
 
 # a wavefront and a workgroup a row, one, four and eight chunks a thread, rows gone over again; ends inside of chunks
-SHAPES = [(1, 1), (3, 5), (9, 8), (5, 77), (13, 512), (7, 513), (5, 2048), (1030, 2000), (1025, 2048), (8, 2049), (3, 8192), (9, 8193), (2, 16384), (3, 16391), (2, 20011)]
+SHAPES = [(1, 1), (3, 5), (9, 8), (5, 77), (13, 512), (7, 513), (5, 2048), (1030, 2000), (1025, 2048), (8, 2049), (3, 8192), (9, 8193), (2, 16384), (3, 16391), (2, 20011),
+          (2048, 2050), (2500, 4096), (1030, 4500), (1025, 8191)]   # (rows in turn)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
