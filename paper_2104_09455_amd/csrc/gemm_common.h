@@ -1001,6 +1001,89 @@ __device__ __forceinline__ void add_residual(typename Mma<CFG::DT, CFG::MI>::Acc
         }
 }
 
+// EPI_ADD of wavefront tiles that, floats and residual at once, are more than registers hold (128 x 64 of the 256 x 256 tile): scaled, activated,
+// added and stored row by row, the residual two block rows ahead.  (One path for whole tiles and those that C cuts: a second one beside it
+// spills 420 registers.  In place as the others, 42 spilled / so, us: 2815 x 11072 x 1664 113 / 91, with GELU 130 / 104, 8192 x 4096 x 2048 with
+// SiLU 154 / 114, 4096 x 4096 x 12288 234 / 223; the smaller tiles are faster in place: 1157 x 1600 x 256 13.4 / 20, 3000 x 2100 x 1024 24.5 / 29.5.)
+template <class CFG>
+constexpr bool residual_by_rows() { return CFG::EPI == EPI_ADD && CFG::INTERLEAVED && CFG::TM * Mma<CFG::DT, CFG::MI>::NACC * CFG::TN > 64; }
+template <class CFG>
+struct ResidualRuns {
+    typedef Mma<CFG::DT, CFG::MI> MMA;
+    static constexpr int TN = CFG::TN, AHEAD = 2;   // block rows
+    typedef int Run __attribute__((ext_vector_type(TN / 2)));
+    struct __attribute__((packed, aligned(2))) AnyRun { Run v; };
+    Run v[AHEAD][MMA::NACC];
+    f32x4 scale[AHEAD][MMA::NACC / 4];
+    bool whole;   // in columns
+    int left;     // columns of C from this lane's first on
+    static __device__ __forceinline__ int half(const Run& w, int j) {
+        if constexpr (TN == 2) return bitcast<int>(w);
+        else return w[j / 2];
+    }
+    __device__ __forceinline__ void load(const GemmArgs& p, const TileCoords<CFG>& tc, int i) {
+#pragma unroll
+        for (int r = 0; r < MMA::NACC; r += 4) scale[i % AHEAD][r / 4] = row_scales(p, tc.row(i, r));
+#pragma unroll
+        for (int r = 0; r < MMA::NACC; ++r) {
+            const char* const row = p.res + min(tc.row(i, r), p.M - 1) * (p.ldr * 2);
+            if (whole) {
+                v[i % AHEAD][r] = load_global_unaligned<Run>(row + (long long)tc.col(0) * 2);
+            } else {
+                unsigned e[TN];
+#pragma unroll
+                for (int j = 0; j < TN; ++j) e[j] = *reinterpret_cast<const unsigned short*>(row + (long long)min(tc.col(j), p.N - 1) * 2);
+                if constexpr (TN == 2) v[i % AHEAD][r] = bitcast<Run>((int)(e[0] | e[1] << 16));
+                else v[i % AHEAD][r] = Run{(int)(e[0] | e[1] << 16), (int)(e[2] | e[3] << 16)};
+            }
+        }
+    }
+    __device__ __forceinline__ void store(const typename MMA::Acc (&acc)[CFG::TM][TN], const GemmArgs& p, const TileCoords<CFG>& tc) {
+        whole = tc.bn0 + (__builtin_amdgcn_readfirstlane(tc.wave_n) + 1) * CFG::WN <= p.N;
+        left = p.N - tc.col(0);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) load(p, tc, i);
+        float col[TN], bias[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int n = min(tc.col(j), p.N - 1);
+            col[j] = p.col_scale[n];
+            bias[j] = p.bias ? p.bias[n] : 0.f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        with_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < CFG::TM; ++i) {
+#pragma unroll
+                for (int r = 0; r < MMA::NACC; ++r) {
+                    const int row = tc.row(i, r);
+                    const float by = scale[i % AHEAD][r / 4][r & 3];
+                    Run out;
+#pragma unroll
+                    for (int j = 0; j < TN; j += 2) {
+                        const int w = half(v[i % AHEAD][r], j);
+                        const float a = act(scaled_value(acc[i][j][r], by, col[j], bias[j], 0));
+                        const float b = act(scaled_value(acc[i][j + 1][r], by, col[j + 1], bias[j + 1], 0));
+                        const int both = pack_out16<CFG::OUT>(mul_add_half<CFG::OUT, 0>(w, 1.f, a), mul_add_half<CFG::OUT, 1>(w, 1.f, b));
+                        if constexpr (TN == 2) out = bitcast<Run>(both);
+                        else out[j / 2] = both;
+                    }
+                    char* const dst = p.C + row * (p.ldc * 2) + (long long)tc.col(0) * 2;
+                    if (row < p.M && left >= TN) {
+                        reinterpret_cast<AnyRun*>(dst)->v = out;
+                    } else if (row < p.M) {
+#pragma unroll
+                        for (int j = 0; j < TN - 1; ++j)
+                            if (j < left) reinterpret_cast<short*>(dst)[j] = (short)(half(out, j) >> (16 * (j & 1)));
+                    }
+                }
+                if (i + AHEAD < CFG::TM) load(p, tc, i + AHEAD);
+                __builtin_amdgcn_sched_barrier(0);   // (more at once than the registers hold)
+            }
+        });
+    }
+};
+
 // EPI_GATED: the wavefront tile's elements of C, half as many columns as the product's (floats already), rounded and stored
 template <class CFG>
 __device__ __forceinline__ void store_gated(typename Mma<CFG::DT, CFG::MI>::Acc (&acc)[CFG::TM][CFG::TN], const GemmArgs& p,
@@ -1263,6 +1346,10 @@ __device__ __forceinline__ void epilogue(typename Mma<CFG::DT, CFG::MI>::Acc (&a
     }
 
     if (!store) return;
+    if constexpr (residual_by_rows<CFG>()) {
+        ResidualRuns<CFG>().store(acc, p, tc);
+        return;
+    }
     if constexpr (CFG::SCALED) {
         scale_tile<CFG>(acc, p, tc);
         if constexpr (CFG::EPI == EPI_ADD) add_residual<CFG>(acc, p, tc);
