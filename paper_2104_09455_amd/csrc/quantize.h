@@ -164,6 +164,7 @@ inline hipError_t launch_quantize_rows(const QuantizeArgs& a, hipStream_t stream
     else if (a.K <= 2048 && a.M >= 1024) { kern = quantize_rows_kernel<DT, 64, 4>; rows = 4; }
     else if (a.K <= 2048) kern = quantize_rows_kernel<DT, 256, 1>;
     else if (a.K <= 8192) kern = quantize_rows_kernel<DT, 256, 4>;
+    else if (a.K <= 16384) kern = quantize_rows_kernel<DT, 256, 8>;   // (4096 x 12288 39.5 us read twice, so 25.3)
     else kern = quantize_rows_kernel<DT, 256, 0>;
     // (a launch holds fewer than 2^32 threads)
     constexpr long long BLOCKS = 1 << 23;

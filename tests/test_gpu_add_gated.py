@@ -425,3 +425,14 @@ def test_small_layers_in_one_launch(M, N, K, dtype, kind):
 
 def bits16(x):
     return x.contiguous().view(torch.int16)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("M,K", [(1, 8200), (5, 12288), (300, 16384), (3, 16385)])
+def test_long_rows_are_quantised_exactly(M, K, dtype):
+    """The rows of down projections: held in registers up to 16384 values, beyond that read twice."""
+    _, t, _, _ = TYPES[dtype]
+    x = hard_rows(M, K, t, seed=M + K)
+    q, scale = run_quantize(x, K, K)
+    want, want_scale = quantised(x)
+    assert torch.equal(scale, want_scale) and torch.equal(q.double(), want)
