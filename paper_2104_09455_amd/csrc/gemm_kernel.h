@@ -252,6 +252,11 @@ void gemm_kernel(const GemmArgs p) {
             }
         }
     };
+    // Weights K x N of int8 products onto a residual or gated: row n's 16-byte chunk c of the B tile at c ^ (n / 4 % 8), so that the eight-byte
+    // pieces of columns four apart, which a turned unit writes side by side, meet half as many others in a bank.  (Four apart they are 16
+    // banks apart: conflicts were 28 % of the cycles of 511 x 2000 x 2047.  us: 333 x 1000 x 2047 15.6 -> 14.8, 20 x 2000 x 2047 11.2 -> 10.5, 2000 x 4000 x
+    // 4000 75 -> 70.)
+    constexpr bool SWIZZLED = ESIZE == 1 && CFG::EPI != EPI_SCALE && (LD == LD_TURN || LD == LD_TURN_RUNS);
     // units of the transposing loader, turned on the way to LDS
     auto store_turned = [&](char* bs, int kt, const i32x4(&rb)[NB]) {
         const bool cut = (kt + 1) * BK > K;
@@ -293,7 +298,8 @@ void gemm_kernel(const GemmArgs p) {
                     c[3][h] = (int)__builtin_amdgcn_perm(y23, y01, 0x07060302u);
                 }
 #pragma unroll
-                for (int n = 0; n < 4; ++n) *reinterpret_cast<i32x2*>(bs + (nl + n) * STRIDE + kl) = c[n];
+                for (int n = 0; n < 4; ++n)
+                    *reinterpret_cast<i32x2*>(bs + (nl + n) * STRIDE + (SWIZZLED ? (((kl >> 4) ^ ((nl >> 2) & 7)) << 4) + (kl & 15) : kl)) = c[n];
             }
         }
     };
@@ -434,7 +440,12 @@ void gemm_kernel(const GemmArgs p) {
                 a[i] = *reinterpret_cast<const i32x4*>(as + i * MI * STRIDE + kk * MMA::KBYTES);
 #pragma unroll
             for (int j = 0; j < TN; ++j)
-                b[j] = *reinterpret_cast<const i32x4*>(bs + j * MI * STRIDE + kk * MMA::KBYTES);
+                if constexpr (SWIZZLED) {
+                    const int n = wave_n * CFG::WN + j * MI + lrow;
+                    b[j] = *reinterpret_cast<const i32x4*>(bs - lgrp * 16 + j * MI * STRIDE + (((kk * MMA::KBYTES / 16 + lgrp) ^ ((n >> 2) & 7)) << 4));
+                } else {
+                    b[j] = *reinterpret_cast<const i32x4*>(bs + j * MI * STRIDE + kk * MMA::KBYTES);
+                }
 #pragma unroll
             for (int i = 0; i < TM; ++i)
 #pragma unroll
