@@ -1,4 +1,5 @@
-"""ctypes binding of libabft.so: the same entry points as include/abft.h.
+"""Binding of libabft.so: the same entry points as include/abft.h, through ctypes (those that a decoding step calls
+between its int8 products through csrc/marshal.c, compiled).
 
 Argument marshalling only -- every step of the path runs in the library's HIP
 kernels.  Tensors are PyTorch device tensors (PyTorch is used for device memory
@@ -206,6 +207,24 @@ def lib() -> ctypes.CDLL:
     L.abft_attention_workspace_bytes.argtypes = [cp, ci, ci, ci, ci, ci, ci]
     _lib = L
     return L
+
+
+_marshal = None
+
+
+def _compiled():
+    """The compiled marshalling of the calls between a decoding step's products (csrc/marshal.c), on the library's entry points."""
+    global _marshal
+    if _marshal is None:
+        L = lib()
+        try:
+            from . import _marshal as m
+        except ImportError as e:
+            raise RuntimeError(f"{HERE}/_marshal.so is missing: build it with `python -m paper_2104_09455_amd.build`") from e
+        m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.abft_gemm_scaled_add, L.abft_linear_scaled_add, L.abft_gemm_gated,
+                                                                 L.abft_linear_gated, L.abft_rms_norm)))
+        _marshal = m
+    return _marshal
 
 
 class AbftError(RuntimeError):
@@ -508,41 +527,32 @@ def abft_linear_scaled(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias
 def abft_gemm_scaled_add(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, R, ldr, C, ldc, out_dtype, mode, beta=None,
                          workspace=None, workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None,
                          stream=None) -> None:
-    ip = ctypes.byref(inject) if inject is not None else None
-    _check(lib().abft_gemm_scaled_add(M, N, K, _ptr(A), lda, _ptr(row_scale), _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act,
-                                      _ptr(R), ldr, _ptr(C), ldc, out_dtype, mode, _ptr(beta), _ptr(workspace), workspace_bytes,
-                                      _ptr(fault_flag), _ptr(report), ip, _stream(stream)))
+    _check(_compiled().gemm_scaled_add(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, R, ldr, C, ldc, out_dtype, mode, beta,
+                                       workspace, workspace_bytes, fault_flag, report, inject, _stream(stream)))
 
 
 def abft_linear_scaled_add(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, R, ldr, C, ldc, mode, beta=None, workspace=None,
                            workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None, stream=None) -> None:
-    ip = ctypes.byref(inject) if inject is not None else None
-    _check(lib().abft_linear_scaled_add(M, N, K, _ptr(X), ldx, dtype, _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act, _ptr(R),
-                                        ldr, _ptr(C), ldc, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag),
-                                        _ptr(report), ip, _stream(stream)))
+    _check(_compiled().linear_scaled_add(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, R, ldr, C, ldc, mode, beta, workspace,
+                                         workspace_bytes, fault_flag, report, inject, _stream(stream)))
 
 
 def abft_gemm_gated(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, beta=None,
                     workspace=None, workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None,
                     stream=None) -> None:
-    ip = ctypes.byref(inject) if inject is not None else None
-    _check(lib().abft_gemm_gated(M, N, K, _ptr(A), lda, _ptr(row_scale), _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act,
-                                 _ptr(C), ldc, out_dtype, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag),
-                                 _ptr(report), ip, _stream(stream)))
+    _check(_compiled().gemm_gated(M, N, K, A, lda, row_scale, B, ldb, b_layout, col_scale, bias, act, C, ldc, out_dtype, mode, beta, workspace,
+                                  workspace_bytes, fault_flag, report, inject, _stream(stream)))
 
 
 def abft_linear_gated(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, C, ldc, mode, beta=None, workspace=None,
                       workspace_bytes=0, fault_flag=None, report=None, inject: Optional[Fault] = None, stream=None) -> None:
-    ip = ctypes.byref(inject) if inject is not None else None
-    _check(lib().abft_linear_gated(M, N, K, _ptr(X), ldx, dtype, _ptr(B), ldb, b_layout, _ptr(col_scale), _ptr(bias), act, _ptr(C),
-                                   ldc, mode, _ptr(beta), _ptr(workspace), workspace_bytes, _ptr(fault_flag), _ptr(report), ip,
-                                   _stream(stream)))
+    _check(_compiled().linear_gated(M, N, K, X, ldx, dtype, B, ldb, b_layout, col_scale, bias, act, C, ldc, mode, beta, workspace, workspace_bytes,
+                                    fault_flag, report, inject, _stream(stream)))
 
 
 def abft_rms_norm(M, K, X, ldx, dtype, weight, eps, residual=None, ldr=0, total=None, ldt=0, Y=None, ldy=0, Q=None, ldq=0, scale=None,
                   stream=None) -> None:
-    _check(lib().abft_rms_norm(M, K, _ptr(X), ldx, dtype, _ptr(weight), eps, _ptr(residual), ldr, _ptr(total), ldt, _ptr(Y), ldy, _ptr(Q),
-                               ldq, _ptr(scale), _stream(stream)))
+    _check(_compiled().rms_norm(M, K, X, ldx, dtype, weight, eps, residual, ldr, total, ldt, Y, ldy, Q, ldq, scale, _stream(stream)))
 
 
 def abft_scaled_select(M, N, K, aligned=True) -> int:

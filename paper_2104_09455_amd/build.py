@@ -3,19 +3,21 @@
     python -m paper_2104_09455_amd.build        # or: from paper_2104_09455_amd.build import build
 
 Each .hip file under csrc/ is compiled to an object in parallel, then linked into
-paper_2104_09455_amd/libabft.so.
+paper_2104_09455_amd/libabft.so; csrc/marshal.c becomes paper_2104_09455_amd/_marshal.so.
 """
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libabft.so")
+MARSHAL = os.path.join(HERE, "_marshal.so")   # the binding's compiled part
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -43,8 +45,18 @@ def _compile(src: str) -> str:
     return obj
 
 
+def build_marshal() -> str:
+    """The compiled part of the Python binding (host code only)."""
+    cmd = [os.environ.get("CC", "gcc"), "-O2", "-shared", "-fPIC", "-Wall", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "marshal.c"), "-o", MARSHAL]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{cmd[0]} failed for marshal.c:\n{r.stderr}")
+    return MARSHAL
+
+
 def build(verbose: bool = False, jobs: int = 8) -> str:
     os.makedirs(OBJDIR, exist_ok=True)
+    build_marshal()
     with ThreadPoolExecutor(max_workers=jobs) as ex:
         objs = list(ex.map(_compile, SOURCES))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
