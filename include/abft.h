@@ -61,7 +61,8 @@ extern "C" {
  * checksum of B_t.  F16 / BF16: the matrix unit adds the fragments of B_t, A.(b_0 + b_1) = A.b_0 +
  * A.b_1, each product into checksum accumulators of its own: the MFMAs of replication (Sec. 5.1),
  * and a checksum side that rounds exactly as the product does.  I8: the sums are formed on the
- * vector unit and handed on in two digits, two MFMAs per A fragment.  AUTO: whatever abft_select
+ * vector unit and handed on in two digits, two MFMAs per A fragment; scaled products (abft_gemm_scaled and what is built on
+ * it): like F16, on exact sums.  AUTO: whatever abft_select
  * returns (intensity-guided ABFT, Sec. 5.3). */
 typedef enum {
     ABFT_NONE = 0,

@@ -514,10 +514,13 @@ struct ChecksumDot {
 };
 
 // Which form of the tile checksum a configuration uses, how many checksum accumulator blocks
-// (and MFMAs a k step) that takes per A fragment.
+// (and MFMAs a k step) that takes per A fragment.  Scaled products issue every product twice, as the 16-bit types do: as many MFMAs as
+// digits take with two fragments of B, twice as many with four, and no vector work, which is what bounds the digits (gated, thread-level,
+// us, digits / here: 1000 x 5000 x 1000 K x N 41 / 24, 256 x 4096 x 4096 17.5 / 13.8, four fragments 1024 x
+// 8192 x 2048 58 / 37, 4096 x 8192 x 4096 383 / 229; unprotected 20, 11.2, 23, 117).
 template <class CFG>
 struct ChecksumForm {
-    static constexpr bool DIGITS = CFG::DT == DT_I8 && CFG::TN >= 2;
+    static constexpr bool DIGITS = CFG::DT == DT_I8 && CFG::TN >= 2 && !CFG::SCALED;
     static constexpr int NP = DIGITS ? 2 : CFG::TN;
     static constexpr int NCHK = NP * CFG::TM;
 };
