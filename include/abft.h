@@ -507,7 +507,7 @@ int abft_rms_norm(int M, int K, const void *X, int64_t ldx, int dtype, const flo
  *   act: any abft_act_t.
  *   mode: ABFT_AUTO is ABFT_THREAD for up to sixteen rows of weights in ABFT_B_NK order with 16-byte aligned rows (ldb below 2^26) and
  *        K of 513 .. 16384, a multiple of 16: such products, unprotected or under ABFT_THREAD, have a kernel of their own (which compares
- *        blocks of 16 x 16; with a report, or a fault at k_after >= 0, they run on the tilings).  So it is in the linear form for K of
+ *        blocks of 16 x 16; with a report, a fault at k_after >= 0, or K >= 8192 and fewer than K / 4 columns of B, they run on the tilings).  So it is in the linear form for K of
  *        16 .. 1024 and at most 256 tiles of 32 x 64 (of either layout and any alignment; K x N: N >= 4, ldb below 2^26).  Else abft_scaled_select.
  * All else, workspaces among it, as there. */
 int abft_gemm_scaled_add(int M, int N, int K, const void *A, int64_t lda, const float *row_scale, const void *B, int64_t ldb,

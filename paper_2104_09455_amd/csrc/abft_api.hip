@@ -1228,7 +1228,11 @@ const ScaledLaunches& scaled_launches(const Problem& pr) {
 }
 
 // Does the kernel of resident activations take this product?  (its THREAD compares 16 x 16 blocks; a report counts the tilings' own)
+// Not a few columns of a long k loop, which the streaming tiles' four to eight wavefronts have more of on its way (tilings / here, us, gated int8, five
+// rows: 256 x 12672 8.0 / 10.0, 1024 x 12672 8.1 / 10.1, 2048 x 12672 11.9 / 12.6, 256 x 8192 6.1 / 6.1, quantised first 8.9 / 10.2; 512 x 4096
+// 4.4 / 4.3, quantised first 7.2 / 6.7; 4096 x 12288 added 17.8 / 14.7).
 bool resident_takes(const Problem& pr, int mode, const abft_report_t* report, const abft_fault_t* inject) {
+    if (pr.K >= 8192 && pr.N < pr.K / 4) return false;
     return pr.epi != EPI_SCALE && (mode == ABFT_NONE || mode == ABFT_THREAD) && b_vectorisable(pr) && resident_fits(pr.M, pr.K) && pr.ldb < (1 << 26) && !report &&
            (!inject || inject->k_after < 0);
 }
