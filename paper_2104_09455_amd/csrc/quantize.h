@@ -85,8 +85,8 @@ __device__ __forceinline__ i32x2 quantize_chunk(const i32x4& v, const GroupScale
 
 // up to eight 16-bit values of a row from element k on (k < K), zeros behind its end; at any address
 __device__ __forceinline__ i32x4 row_chunk16(const char* row, int k, int K) {
-    if (k + 8 <= K) return ld16u(row + 2ll * k);
-    if (K >= 8) return shift_down(ld16u(row + 2ll * (K - 8)), 2 * (k + 8 - K));
+    if (k <= K - 8) return ld16u(row + 2ll * k);   // (k + 8 may pass 32 bits)
+    if (K >= 8) return shift_down(ld16u(row + 2ll * (K - 8)), 2 * (k - (K - 8)));
     return gather16<2>(row + 2ll * k, 2, K - k);
 }
 
