@@ -71,7 +71,7 @@ __device__ __forceinline__ void weights(const float* w, int k, int K, float (&f)
     if (!w) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = 1.f;
-    } else if (k + 8 <= K) {
+    } else if (k <= K - 8) {
         const f32x4 a = load_global_unaligned<f32x4>(reinterpret_cast<const char*>(w + k));
         const f32x4 b = load_global_unaligned<f32x4>(reinterpret_cast<const char*>(w + k + 4));
 #pragma unroll
@@ -94,6 +94,8 @@ __device__ __forceinline__ i32x4 norm_chunk(const i32x4& s, float lift, float in
     for (int d = 0; d < 4; ++d) y[d] = pack_out16<DT>(f[2 * d] * lift * inv * w[2 * d], f[2 * d + 1] * lift * inv * w[2 * d + 1]);
     return y;
 }
+
+constexpr float LIFT = 0x1p-80f;   // (its square is no float)
 
 // DT: the type of the values; TPR threads share a row and hold it (NV chunks of eight values each); with NV = 0 they go over it again
 template <int DT, int TPR, int NV>
@@ -123,6 +125,7 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(const NormArgs p) {
     };
     i32x4 v[NV ? NV : 1];
     float total = 0.f;
+    double many = 0.;   // (a thread's chunks of a row that is not held: up to 2^20 of them)
     if constexpr (NV != 0) {
         i32x4 a[NV], b[NV];
 #pragma unroll
@@ -142,27 +145,30 @@ __global__ __launch_bounds__(256) void rms_norm_kernel(const NormArgs p) {
         for (long long k = t * 8; k < K; k += TPR * 8) {
             const i32x4 c = chunk((int)k);
             if (s) store_chunk(s + 2 * k, c, (int)(K - k));
-            total = square_chunk<DT>(c, 1.f, total);
+            many += square_chunk<DT>(c, 1.f, 0.f);
         }
+        total = (float)many;
     }
     // (the sum may lie where an operand was: from here on it is read, by the thread that wrote it)
     auto again = [&](int k) { return s ? row_chunk16(s, k, K) : chunk(k); };
     total = row_sum(total);
-    float lift = 1.f;
-    if (DT == DT_BF16 && !(total < __builtin_huge_valf())) {
+    float lift = 1.f, mean = total / (float)K + p.eps;
+    if (DT == DT_BF16 && !(mean < __builtin_huge_valf())) {
         // squares of bf16 values above 2^64 are no floats: once more, 2^80 smaller (fp16 has none)
-        lift = 0x1p-80f;
+        lift = LIFT;
         total = 0.f;
         if constexpr (NV != 0) {
 #pragma unroll
             for (int c = 0; c < NV; ++c) total = square_chunk<DT>(v[c], lift, total);
         } else {
-            for (long long k = t * 8; k < K; k += TPR * 8) total = square_chunk<DT>(again((int)k), lift, total);
+            many = 0.;
+            for (long long k = t * 8; k < K; k += TPR * 8) many += square_chunk<DT>(again((int)k), lift, 0.f);
+            total = (float)many;
         }
         if constexpr (TPR == 256) __syncthreads();   // (everyone has read the first sums)
-        total = row_sum(total);
+        mean = row_sum(total) / (float)K + p.eps * LIFT * LIFT;
     }
-    const float inv = 1.f / __builtin_sqrtf(total / (float)K + p.eps * (lift * lift));
+    const float inv = 1.f / __builtin_sqrtf(mean);
     int top = 0;
     auto normed = [&](int k, const i32x4& c) {
         float w[8];
@@ -243,9 +249,9 @@ __global__ __launch_bounds__(256) void rms_norm_rows_kernel(const NormArgs p) {
         if ((tid & 63) == 0) sums[buf][tid >> 6] = total;
         __syncthreads();
         total = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
-        float lift = 1.f;
-        if (DT == DT_BF16 && !(total < __builtin_huge_valf())) {
-            lift = 0x1p-80f;
+        float lift = 1.f, mean = total / (float)K + p.eps;
+        if (DT == DT_BF16 && !(mean < __builtin_huge_valf())) {
+            lift = LIFT;
             total = 0.f;
 #pragma unroll
             for (int c = 0; c < NV; ++c) total = square_chunk<DT>(v[c], lift, total);
@@ -253,9 +259,9 @@ __global__ __launch_bounds__(256) void rms_norm_rows_kernel(const NormArgs p) {
             __syncthreads();   // (everyone has read the first sums)
             if ((tid & 63) == 0) sums[buf][tid >> 6] = total;
             __syncthreads();
-            total = (sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3]);
+            mean = ((sums[buf][0] + sums[buf][1]) + (sums[buf][2] + sums[buf][3])) / (float)K + p.eps * LIFT * LIFT;
         }
-        const float inv = 1.f / __builtin_sqrtf(total / (float)K + p.eps * (lift * lift));
+        const float inv = 1.f / __builtin_sqrtf(mean);
         int top = 0;
 #pragma unroll
         for (int c = 0; c < NV; ++c) {

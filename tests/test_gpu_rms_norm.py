@@ -161,6 +161,19 @@ def test_eps_counts_where_rows_are_small():
         check(y, x.rows, None, "bf16", eps)
 
 
+@pytest.mark.parametrize("M,K", [(3, 96), (5, 1000), (2, 8192), (2, 20000), (2048, 4096)])
+def test_mean_and_eps_that_are_no_float_together(M, K):
+    """The mean of squares and eps are floats, their sum is not; and eps beside a mean that is none counts."""
+    g = torch.Generator().manual_seed(K)
+    x = Rows(((torch.rand(M, K, generator=g) * 0.5 + 1.0) * 2.0 ** 63).to(torch.bfloat16))
+    for eps in (3.4e38, 3e38, 1e38):
+        y, _ = run(x, "bf16", K, eps=eps)
+        check(y, x.rows, None, "bf16", eps)
+    x = Rows(((torch.rand(M, K, generator=g) * 0.5 + 1.0) * 2.0 ** 65).to(torch.bfloat16))
+    y, _ = run(x, "bf16", K, eps=3.4e38)
+    check(y, x.rows, None, "bf16", 3.4e38)
+
+
 def test_more_rows_than_a_launch_holds():
     """2^25 rows, four a workgroup."""
     M, K = (1 << 25) + 5, 3
