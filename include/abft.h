@@ -610,7 +610,8 @@ const char *abft_strerror(int code);
 /* Library version, e.g. 100 = 1.0.0. */
 int abft_version(void);
 /* Measurement hook: two hipEvent_t handles (cast to void*) that the following abft_gemm /
- * abft_conv / abft_plan_run / abft_gemm_scaled / abft_linear_scaled calls of the calling host thread record on their
+ * abft_conv / abft_plan_run / abft_gemm_scaled / abft_linear_scaled calls, and those of the latter's forms with a residual or
+ * gates, of the calling host thread record on their
  * stream immediately before and after launching the matrix-product kernel itself (not the
  * checksum pre-pass, the comparison or the quantisation, but where the product's kernel quantises its few rows itself, that too).
  * NULL, NULL switches it off. */
