@@ -169,6 +169,14 @@ hipError_t launch_resident_add_bf16(bool checked, bool from16, const GemmArgs& a
 hipError_t launch_resident_gated_f16(bool checked, bool from16, const GemmArgs& args, hipStream_t stream);
 hipError_t launch_resident_gated_bf16(bool checked, bool from16, const GemmArgs& args, hipStream_t stream);
 constexpr int resident_tiles(int k) { return k <= 8192 ? (k + 1023) / 1024 : (k + 2047) / 2048 * 2; }
+// A wavefront's first k tile of a row's nkt, and where in its part of the row (`left` values to the row's end) it reads 16 bytes of its tile t:
+// chunks beyond K are read from the row's last 16.  Tiles before the last that every wavefront owns lie inside of K, and are read as they lie:
+// a wavefront owns at least tiles - 1 of them, beyond 8192 values of k, where `tiles` is rounded up to an even number, tiles - 2.
+constexpr int resident_first(int nkt, int wave) { return wave * (nkt / 8) + (wave < nkt % 8 ? wave : nkt % 8); }
+constexpr bool resident_whole(int tiles, int t) { return t < tiles - (tiles <= 8 ? 2 : 3); }
+constexpr int resident_at(int tiles, int t, int chunk, int left) {
+    return resident_whole(tiles, t) || t * 128 + chunk < left - 16 ? t * 128 + chunk : left - 16;
+}
 constexpr bool resident_fits(int rows, int k) { return rows <= 16 && k > 512 && k <= 16384; }
 
 }  // namespace abft

@@ -14,6 +14,7 @@
 // 4096 7.6 / 5.6, 16 rows of it 10.4 / 8.7; pre-quantised gated 16 x 8192 x 4096 19.6 / 18.5, 16 x 8192 x 8192 33.1 / 29.9.  Two blocks of
 // sixteen rows, level to 8 % ahead from 4096 values of k on and 10 to 30 % behind below, and four, behind by a fifth, were left to the tilings.
 #pragma once
+#include "gemm_configs.h"
 #include "quantize.h"
 
 namespace abft {
@@ -52,7 +53,7 @@ __global__ __launch_bounds__(64 * RES_WAVES, (T <= 4 ? 4 : 2)) void gemm_residen
     const int M = p.M, N = p.N, K = p.K;
     // this wavefront's k tiles: a run of them, of a row's nkt
     const int nkt = (K + 127) >> 7, share = nkt / W, more = nkt % W;
-    const int n_own = share + (wave < more ? 1 : 0), k0 = (wave * share + min(wave, more)) * 128;   // (k0 = nkt * 128 without one)
+    const int n_own = share + (wave < more ? 1 : 0), k0 = resident_first(nkt, wave) * 128;   // (k0 = nkt * 128 without one)
     // this workgroup's columns, by the sixteen (runs of workgroups of one die are runs of columns)
     const int wgs = (int)gridDim.x;
     int lin = (int)blockIdx.x;
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(64 * RES_WAVES, (T <= 4 ? 4 : 2)) void gemm_residen
 
     // (k tiles beyond this wavefront's, and chunks beyond K, are multiplied with zeros of A: any place in the row will do)
     i32x4 v[D][2];
-    // (a base for all lanes, a lane's own 32 bits, and a constant: only a wavefront's last two k tiles may leave its k)
+    // (a base for all lanes, a lane's own 32 bits, and a constant where the tile is a whole one)
     const char* base;
     unsigned rows[2];
     auto columns = [&](int col0) {
@@ -70,10 +71,14 @@ __global__ __launch_bounds__(64 * RES_WAVES, (T <= 4 ? 4 : 2)) void gemm_residen
         for (int q = 0; q < 2; ++q) rows[q] = (unsigned)min(q * 8 + crow, last - 1 - col0) * (unsigned)p.ldb;
     };
     auto fetch = [&](int slot, int t) {
+        // (beyond eight k tiles worked out where it is used, since the registers are full: kept / so, us, from memory, 1 x 4096 x 12288 added 14.1 / 13.4,
+        // 16 x 4096 x 16384 21.3 / 20.3, from integers 17.3 / 16.1; unprotected level, 4 x 4096 x 16384 18.6 / 18.8)
+        int c = chunk;
+        if (T > RES_DEEP && !resident_whole(T, t)) asm volatile("" : "+v"(c));
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            if (t < T - 2) v[slot][q] = ld16g(base + (rows[q] + (unsigned)chunk) + t * 128);
-            else v[slot][q] = ld16g(base + (int)(rows[q] + (unsigned)min(t * 128 + chunk, K - 16 - k0)));
+            if (resident_whole(T, t)) v[slot][q] = ld16g(base + (rows[q] + (unsigned)chunk) + t * 128);
+            else v[slot][q] = ld16g(base + (int)(rows[q] + (unsigned)resident_at(T, t, c, K - k0)));
         }
     };
     // the turn of sixteen rows of 128 bytes: whole lines in, fragments out (a wavefront's LDS operations execute in order)
