@@ -1237,7 +1237,7 @@ bool resident_takes(const Problem& pr, int mode, const abft_report_t* report, co
            (!inject || inject->k_after < 0);
 }
 // Does the kernel that quantises and multiplies in one launch take this layer of 16-bit activations?  (One round of its workgroups: two launches / so, us,
-// 300 x 1000 x 1000, 160 of them, 10.0 / 8.5, 300 x 2048 x 1024, 320 of them, 10.8 / 14.3.)
+// 300 x 1600 x 1024, 250 of them, 11.3 / 7.4, K x N 9.5 / 8.0; 300 x 2048 x 1024, 320 of them, 13.0 / 13.1, K x N 10.9 / 13.9.)
 bool joint_takes(const Problem& pr, int mode, const abft_report_t* report, const abft_fault_t* inject) {
     return pr.epi != EPI_SCALE && (mode == ABFT_NONE || mode == ABFT_THREAD || mode == ABFT_AUTO) && pr.K >= 16 && pr.K <= JOINT_MAX_K && pr.ldb < (1 << 26) &&
            (pr.b_layout == ABFT_B_NK || pr.N >= 4) && cdiv(pr.M, JOINT_M) * cdiv(pr.N, JOINT_N) <= 256 && !report &&

@@ -12,10 +12,12 @@
 // Checked: every MFMA goes out twice, the second into one block for the four fragments of a row block; its elements and the sum of
 // the four fragments' agree modulo 2^32 (replication with single accumulation, Sec. 5.1), and a flipped bit never changes a sum by a
 // multiple of that.
-// Bound: latencies; at 1024 values of k the quantisation (1 us) and the partial tiles' way through LDS beside them.  Measured, bf16, residual, us in a graph (two
-// launches / so): 16 x 1000 x 1000 5.9 / 7.2, 64 x 512 x 512 6.0 / 6.3, 300 x 1000 x 1000 10.0 / 8.5, K x N 64 x 512 x 512 9.2 / 6.1, 300 x 1000 x 1000
-// 11.5 / 8.9; a launch less is 3.3 us less of the host's time, which is what a program that does not record a graph waits for (a call 8.7 / 5.5).
-// Beyond a round of workgroups the tilings are ahead: 300 x 2048 x 1024 (320 of them) 10.8 / 14.3, 1500 x 512 x 512 (376) 10.3 / 12.0.
+// Bound: latencies; at 1024 values of k the quantisation (1 us) and the partial tiles' way through LDS beside them.  Measured, bf16, residual,
+// thread-level, us in a graph (two launches / so): 16 x 1000 x 1000 5.4 / 6.9, 64 x 512 x 512 5.5 / 5.9, 300 x 1000 x 1000 8.9 / 7.3, K x N
+// 64 x 512 x 512 8.4 / 5.8, 300 x 1000 x 1000 10.1 / 7.9 (unprotected 0.3 less); a launch less is 3.3 us less of the host's time, which is what a
+// program that does not record a graph waits for (calls in a row: 16 x 1000 x 1000 8.7 / 7.2, 64 x 512 x 512 8.3 / 6.4).
+// Beyond a round of workgroups the tilings are level or ahead: 300 x 2048 x 1024 (320 of them) 13.0 / 13.1, K x N 10.9 / 13.9, 1500 x 512 x 512 (376)
+// 12.2 / 10.9, K x N 8.7 / 10.9.
 #pragma once
 #include "quantize.h"
 
@@ -130,7 +132,9 @@ __global__ __launch_bounds__(64 * JOINT_WAVES, 4) void gemm_joint_kernel(const G
     for (int b = 0; b < 2; ++b) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[b][j] = Acc{0, 0, 0, 0};
-        chk[b] = Acc{0, 0, 0, 0};
+        int zero = 0;
+        if constexpr (CHECKED) asm("" : "+v"(zero));   // (or the block would be the first fragment's as far as the two agree, and be merged with it)
+        chk[b] = Acc{zero, 0, 0, 0};
     }
     char* const own = smem + JOINT_M * arow + wave * 2048;   // (N x K)
     int to[2], at[2];
