@@ -289,13 +289,16 @@ __global__ __launch_bounds__(256) void rms_norm_rows_kernel(const NormArgs p) {
     }
 }
 
+// Chunks of eight values that each of 256 threads holds of a row of k
+constexpr int held_chunks(int k) { return (k - 1) / 2048 + 1; }
+
 template <int DT>
 hipError_t launch(const NormArgs& a, hipStream_t stream) {
     void (*kern)(const NormArgs);
     int rows = 1;
     // (a workgroup for each row / rows in turn, us, bf16 with a residual: 8192 x 8192 105 / 98.7, 8192 x 5120 65 / 63, 4096 x 4096 28.5 / 25.5, 2048 x 4096 15.4 / 15.0,
     // 1024 x 8192 16.1 / 15.2; 8192 x 2048 25.2 / 26.2, 8192 x 1024 15.2 / 17.3)
-    const int nv = (a.K + 2047) / 2048, wgs = nv == 2 ? 1024 : 512;   // (as many as their registers let the chip hold)
+    const int nv = held_chunks(a.K), wgs = nv == 2 ? 1024 : 512;   // (as many as their registers let the chip hold)
     if (nv >= 2 && nv <= 4 && a.M >= 2 * wgs) {
         kern = nv == 2 ? rms_norm_rows_kernel<DT, 2> : nv == 3 ? rms_norm_rows_kernel<DT, 3> : rms_norm_rows_kernel<DT, 4>;
         hipLaunchKernelGGL(kern, dim3((unsigned)wgs), dim3(256), 0, stream, a);
