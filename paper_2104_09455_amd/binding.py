@@ -220,7 +220,7 @@ def _compiled():
         try:
             from . import _marshal as m
         except ImportError as e:
-            raise RuntimeError(f"{HERE}/_marshal.so is missing: build it with `python -m paper_2104_09455_amd.build`") from e
+            raise RuntimeError(f"{HERE} has no _marshal module for this interpreter: build it with `python -m paper_2104_09455_amd.build`") from e
         m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (L.abft_gemm_scaled_add, L.abft_linear_scaled_add, L.abft_gemm_gated,
                                                                  L.abft_linear_gated, L.abft_rms_norm)))
         _marshal = m

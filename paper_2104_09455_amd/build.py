@@ -3,7 +3,8 @@
     python -m paper_2104_09455_amd.build        # or: from paper_2104_09455_amd.build import build
 
 Each .hip file under csrc/ is compiled to an object in parallel, then linked into
-paper_2104_09455_amd/libabft.so; csrc/marshal.c becomes paper_2104_09455_amd/_marshal.so.
+paper_2104_09455_amd/libabft.so; csrc/marshal.c becomes the extension module
+paper_2104_09455_amd/_marshal.<interpreter>.so.
 """
 from __future__ import annotations
 
@@ -17,7 +18,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJDIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libabft.so")
-MARSHAL = os.path.join(HERE, "_marshal.so")   # the binding's compiled part
+MARSHAL = os.path.join(HERE, "_marshal" + sysconfig.get_config_var("EXT_SUFFIX"))   # the binding's compiled part, for this interpreter
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -51,6 +52,9 @@ def build_marshal() -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"{cmd[0]} failed for marshal.c:\n{r.stderr}")
+    untagged = os.path.join(HERE, "_marshal.so")   # (as it was called before: any interpreter would load it)
+    if os.path.exists(untagged):
+        os.remove(untagged)
     return MARSHAL
 
 
