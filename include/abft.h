@@ -468,8 +468,8 @@ int abft_gemm_scaled(int M, int N, int K, const void *A, int64_t lda, const floa
                      int mode, const void *beta, void *workspace, size_t workspace_bytes, uint32_t *fault_flag,
                      abft_report_t *report, const abft_fault_t *inject, void *stream);
 
-/* The scheme that ABFT_AUTO stands for in these calls: by measurement the faster protected one (`aligned` as for abft_region_shape), but for up to
- * 64 rows of weights of some 10^8 bytes and more, where ABFT_THREAD is up to 14 % ahead of it.
+/* The scheme that ABFT_AUTO stands for in these calls: by measurement the faster protected one (`aligned` as for abft_region_shape), to within
+ * 5 % where the two are level, but for up to 64 rows of weights of some 10^8 bytes and more, where ABFT_THREAD is up to 14 % ahead of it.
  * ABFT_THREAD or ABFT_GLOBAL, or a negative error. */
 int abft_scaled_select(int M, int N, int K, int aligned);
 
@@ -503,7 +503,8 @@ int abft_rms_norm(int M, int K, const void *X, int64_t ldx, int dtype, const flo
 
 /* abft_gemm_scaled and abft_linear_scaled with a residual added behind the activation function, in the same kernel:
  *     C = R + act((A.B) * row_scale * col_scale + bias), one rounding
- *   R  : M x N, ldr >= N, of the type of C.  May be C itself (the same rows); overlaps it in no other way.
+ *   R  : M x N, ldr >= N, of the type of C.  May be C itself (the same rows); overlaps it in no other way.  (In place the sum stands where the
+ *        residual was: a caller who means to repeat a product that raised the flag keeps R apart from C.)
  *   act: any abft_act_t.
  *   mode: ABFT_AUTO is ABFT_THREAD for up to sixteen rows of weights in ABFT_B_NK order with 16-byte aligned rows (ldb below 2^26) and
  *        K of 513 .. 16384, a multiple of 16: such products, unprotected or under ABFT_THREAD, have a kernel of their own (which compares

@@ -836,7 +836,7 @@ int select_mode(int M, int N, int K, int dt) {
     return intensity(M, N, K, dt) > cmr_of(dt) ? ABFT_GLOBAL : ABFT_THREAD;
 }
 // The faster protected scheme of a scaled product.  Aligned, the global one wherever 32 x 32 tiles are more than one per compute unit:
-// beyond 64 x 64 tiles the thread-level one's second MFMA a product costs more than the weight checksums' columns, and before level (bf16 out,
+// beyond 64 x 64 tiles the thread-level one's second MFMA a product costs more than the weight checksums' columns, before it is 3 to 6 % ahead (bf16 out,
 // thread-level / global, us: 64 x 4096 x 4096 7.6 / 8.1, 96 rows 8.7 / 9.0, 256 rows 12.7 / 11.8, 1024 33 / 24; 128 x 2048 x 8192 9.0 / 9.9, 192
 // rows 12.0 / 12.5; 512 x 512 x 512 3.3 / 3.6, 1024 rows 4.4 / 4.6).  Few rows, whole calls with the quantisation, weights from memory: 1 x 8192 x
 // 4096 11.5 / 12.2, 1 x 8224 x 4096 15.3 / 13.7, 4 x 11008 x 4096 16.7 / 15.7, 16 x 14336 x 8192 30.8 / 29.1, 32 x 32000 x 1024 20.0 / 17.2; only
@@ -1228,9 +1228,9 @@ const ScaledLaunches& scaled_launches(const Problem& pr) {
 }
 
 // Does the kernel of resident activations take this product?  (its THREAD compares 16 x 16 blocks; a report counts the tilings' own)
-// Not a few columns of a long k loop, which the streaming tiles' four to eight wavefronts have more of on its way (tilings / here, us, gated int8, five
-// rows: 256 x 12672 8.0 / 10.0, 1024 x 12672 8.1 / 10.1, 2048 x 12672 11.9 / 12.6, 256 x 8192 6.1 / 6.1, quantised first 8.9 / 10.2; 512 x 4096
-// 4.4 / 4.3, quantised first 7.2 / 6.7; 4096 x 12288 added 17.8 / 14.7).
+// Not a few columns of a long k loop, which the streaming tiles' four to eight wavefronts have more of on its way (tilings / here, us, from memory, gated
+// int8, five rows: 256 x 12672 7.6 / 8.8, 1024 x 12672 9.8 / 10.2, 2048 x 12672 10.5 / 10.9, 16-bit rows 14.0 / 14.2; 256 x 8192 6.0 / 6.2, 16-bit rows
+// 8.9 / 10.2; 512 x 4096 4.4 / 4.3, 16-bit rows 7.2 / 6.7; 4096 x 12288 added 17.8 / 14.0).
 bool resident_takes(const Problem& pr, int mode, const abft_report_t* report, const abft_fault_t* inject) {
     if (pr.K >= 8192 && pr.N < pr.K / 4) return false;
     return pr.epi != EPI_SCALE && (mode == ABFT_NONE || mode == ABFT_THREAD) && b_vectorisable(pr) && resident_fits(pr.M, pr.K) && pr.ldb < (1 << 26) && !report &&

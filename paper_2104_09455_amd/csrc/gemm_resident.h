@@ -10,7 +10,7 @@
 // Every product is issued twice where it is checked, into accumulators of its own (thread-level scheme on a tile of one
 // fragment: replication); both sides are equal to the last bit unless something failed.
 // Bound: the weights' bytes.  Measured, from memory, us (the tilings' kernels and a quantisation of its own / here): gated 1 x 12288 x 4096,
-// 100 MB, 41 / 22 (launch and first latency 4, the rest at 5.6 TB/s), 1 x 8192 x 8192 43 / 28; a residual, 1 x 4096 x 12288 17.8 / 14.7, 1 x 4096 x
+// 100 MB, 41 / 22 (launch and first latency 4, the rest at 5.6 TB/s), 1 x 8192 x 8192 43 / 28; a residual, 1 x 4096 x 12288 17.8 / 14.0, 1 x 4096 x
 // 4096 7.6 / 5.6, 16 rows of it 10.4 / 8.7; pre-quantised gated 16 x 8192 x 4096 19.6 / 18.5, 16 x 8192 x 8192 33.1 / 29.9.  Two blocks of
 // sixteen rows, level to 8 % ahead from 4096 values of k on and 10 to 30 % behind below, and four, behind by a fifth, were left to the tilings.
 #pragma once

@@ -2,8 +2,9 @@
 //   s = round(x + r),   y = round(s / sqrt(mean s^2 + eps) * w),   (q, scale) = y quantised as abft_quantize_rows does
 // A row stays in its threads' registers from the sum to the integers, so every value is read and written once.
 // Bound: bytes, 2 K each for x, r, s and y; few rows: a chain of two round trips to memory and two sums over the row.  Measured, bf16, with a
-// residual, both of s and y: 8192 x 8192 95.8 us (5.6 TB/s), 4096 x 4096 25.3, 600 x 5000 7.5, 1 x 4096 3.7 in a graph.  Rows at odd addresses: 1861 x 3789
-// 16.8, where the vector memory path takes 16 bytes a lane off the dword at a quarter of its rate.
+// residual, both of s and y: 8192 x 8192 95.8 us (5.6 TB/s), 4096 x 4096 25.3, 600 x 5000 7.5, 1 x 4096 3.7 in a graph.  Rows off the
+// dword: 1861 x 3789 16.9, at even pitches 15.0, whole 16-byte chunks (3784, 3792) 13.7.  An odd width: 1001 x 2047 without a residual 4.8, 2048 3.9 (the
+// last chunk is stored value by value); every other row off the dword 5.1.
 #include <hip/hip_runtime.h>
 
 #include "../../include/abft.h"
